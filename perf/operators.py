@@ -9,7 +9,7 @@ A case is a dict of plain values.  ``op`` names the operator:
            ``layout`` is the table's: "fp32", "bf16", or "mx4" (MX4.embed)
   grad     Store.embed_grad ("dense") or Store.embed_grad_rows ("rows") of
            ``n`` ids
-  clip     clip_grads of ``tensors`` tensors with ``total`` elements
+  clip     ClipPlan.clip of ``tensors`` tensors with ``total`` elements
   quant    mx4_quantize of a [rows, dim] table, and the values it stands for
   product  mx4_product of ``m`` queries with a table of ``rows`` rows
 
@@ -209,8 +209,10 @@ def prepare(case, seed):
         st["a"] = _packed(_table(g, case["m"], case["dim"], torch.float32))
         st["b"] = _packed(_table(g, case["rows"], case["dim"], torch.float32))
     if own:
-        from paper_2206_00470_amd import MX4, Store
-        if op in ("embed", "grad"):
+        from paper_2206_00470_amd import MX4, ClipPlan, Store
+        if op == "clip":
+            st["plan"] = ClipPlan(st["grads"], st["outs"])
+        elif op in ("embed", "grad"):
             st["table"] = (MX4(st["codes"], st["scales"], case["dim"]) if "codes" in st else
                            Store(st["W"], st["G"]))
         elif op == "product":
@@ -266,7 +268,7 @@ def run(st):
     case = st["case"]
     op = case["op"]
     if own:
-        from paper_2206_00470_amd import clip_grads, mx4_product, mx4_quantize
+        from paper_2206_00470_amd import mx4_product, mx4_quantize
         if op == "embed":
             return st["table"].embed(st["ids"], scale=st["scale"], dtype=TYPES[case["out"]], pad=PAD)
         if op == "grad" and case["form"] == "dense":
@@ -275,7 +277,7 @@ def run(st):
             return st["table"].embed_grad_rows(st["ids"], st["dout"], scale=st["scale"], pad=PAD,
                                                dtype=TYPES[case["out"]])
         if op == "clip":
-            return clip_grads(st["grads"], st["max_norm"], out=st["outs"]), st["flat"]
+            return st["plan"].clip(st["max_norm"]), st["flat"]
         if op == "quant":
             return mx4_quantize(st["x"]).dequantize(TYPES[case["out"]])
         return mx4_product(st["qa"], st["qb"], scale=st["scale"], dtype=TYPES[case["out"]])
