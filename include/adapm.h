@@ -401,6 +401,108 @@ ps_status ps_read_timing(ps_store* s, int32_t kernel_id, double* total_ms, int64
 ps_status ps_probe_gather(ps_store* s, const int32_t* keys, int64_t n, double* sink, void* stream);
 
 /* ======================================================================
+ * A store as a token table: the lookup with scaling of a language model's
+ * first layer, its gradient, the clipping of all gradients by their global
+ * norm, and a copy of the table in 4 bits that lookups and scores are
+ * answered from.
+ *
+ * Element types of activations, gradients and lookups: fp32, bf16, fp16 as
+ * stored.  A padding id `pad` marks occurrences that take no part (any value,
+ * also one outside the table, raises no error); PS_NO_PAD: none.  Rows may be
+ * strided (strides in elements); vectors are used where dim, strides and
+ * addresses allow them, single elements elsewhere. */
+#define PS_F32  0
+#define PS_BF16 1
+#define PS_F16  2
+#define PS_NO_PAD INT64_MIN
+
+/* Lookup with scaling: out[i*out_stride + c] = T(scale * W[ids[i]][c]) for
+ * i < n, the product rounded to fp32 and then to the element type T of out;
+ * a row of zeros where ids[i] == pad.  Ids outside the table give a row of
+ * zeros and raise the sticky error, as in ps_pull.  Every store (fp32 of any
+ * width, row-wise, bf16; staged: resident rows).  ids: device int64[n]; out:
+ * device, out_stride >= dim; must not overlap the table.  No workspace. */
+ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t out_type,
+                   void* out, int64_t out_stride, void* stream);
+
+/* Gradient of the lookup: for every row v of the table
+ *   grad[v] = scale * sum of dout[i] over the i < n with ids[i] == v
+ * zero where there is none: all num_keys rows are written.  With accumulate
+ * != 0 the sums are added to what grad holds, and other rows stay as they
+ * are (the token table's share of a tied gradient).  The occurrences of an id
+ * are summed in fp64 in a fixed order (the same inputs give the same bits),
+ * scaled (and added) in fp64, rounded to fp32 and then to the type of grad.
+ * Reads no table row and changes none.  Ids outside the table take no part
+ * and raise the sticky error.  dout: device [n][dim], row stride dout_stride;
+ * grad: device [num_keys][dim], row stride grad_stride.  Workspace:
+ * ps_embed_grad_workspace_bytes(dim, n) (0: invalid arguments, or n = 0,
+ * which needs none).  Staged stores: PS_ERR_UNSUPPORTED. */
+size_t ps_embed_grad_workspace_bytes(int32_t dim, int64_t n);
+ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+                        const void* dout, int64_t dout_stride, int32_t out_type, void* grad, int64_t grad_stride,
+                        int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* The same gradient as merged rows, for tables much larger than a batch:
+ * uniq (device int64[n]) receives the distinct ids that take part in
+ * ascending order, rows (device [n][dim], row stride rows_stride) their
+ * gradient rows, *num_unique (device int32) their number U; uniq[U..] and
+ * rows[U..] are left as they are.  ps_push takes uniq and rows as they are
+ * (fp32, dense). */
+ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+                             const void* dout, int64_t dout_stride, int32_t out_type, int64_t* uniq, void* rows,
+                             int64_t rows_stride, int32_t* num_unique, void* ws, size_t ws_bytes, void* stream);
+
+/* Global gradient norm of `count` tensors, and clipping by it:
+ *   *norm = sqrt( sum over all tensors k and elements j of grads[k][j]^2 )
+ *   outs[k][j] = T( coef * grads[k][j] ),
+ *   coef = max_norm / *norm (in fp64, rounded to fp32) if *norm > max_norm,
+ *   else 1.
+ * Squares and sums are fp64 in a fixed order.  A norm that is NaN makes every
+ * output NaN; an infinite one makes coef 0 (so the infinite elements NaN).
+ * grads, outs, numel, types: host arrays, read during the call only, of
+ * device addresses, elements and element types (PS_F32, ...); the tensors
+ * are dense, of any size (0 too) and alignment.  outs[k] may be grads[k] (in
+ * place; nothing is written where coef is 1); otherwise outputs must lie
+ * apart from each other and from all inputs (PS_ERR_INVALID).  norm: device
+ * double[1].  Workspace: ps_clip_workspace_bytes(count).  max_norm > 0. */
+size_t ps_clip_workspace_bytes(int32_t count);
+ps_status ps_grad_norm(int32_t count, const void* const* grads, const int64_t* numel, const int32_t* types,
+                       double* norm, void* ws, size_t ws_bytes, void* stream);
+ps_status ps_clip_grads(int32_t count, const void* const* grads, void* const* outs, const int64_t* numel,
+                        const int32_t* types, double max_norm, double* norm, void* ws, size_t ws_bytes, void* stream);
+
+/* Microscaled 4-bit rows: each row of dim values in ceil(dim/32) blocks of 32
+ * (the last filled up with zeros), 16 bytes of codes and one scale byte s a
+ * block.  A code is sign, two exponent bits and one mantissa bit (magnitudes
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6), two codes a byte, the first in the low half;
+ * a value is its code times 2^(s-127), s = 255 marks a block of NaN.
+ * Quantisation: s = max(0, floor(log2 of the block's largest magnitude) - 2 +
+ * 127), codes to the nearest, ties to the even code, at most 6; a block that
+ * holds an infinity or NaN is NaN.  dim in [1, 16384].
+ * x: device [rows][dim] of `type`, row stride row_stride; codes: device
+ * uint8[rows][ceil(dim/32)*16], 16-byte aligned; scales: device
+ * uint8[rows][ceil(dim/32)]. */
+ps_status ps_mx4_quantize(int64_t rows, int32_t dim, int32_t type, const void* x, int64_t row_stride,
+                          uint8_t* codes, uint8_t* scales, void* stream);
+
+/* ps_embed from a quantised table: the value is exact in fp32 (infinite where
+ * it is beyond: s > 252, which no quantisation gives), then scaled and rounded
+ * as there.  ids NULL: the first n rows in order (n <= num_rows).
+ * err: device int32[2], err[0] set to 1 by an id outside [0, num_rows) (never
+ * cleared by this call); may be NULL where ids is. */
+ps_status ps_mx4_embed(const uint8_t* codes, const uint8_t* scales, int64_t num_rows, int32_t dim,
+                       const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t out_type, void* out,
+                       int64_t out_stride, int32_t* err, void* stream);
+
+/* Scores of m quantised queries against n quantised rows of the same dim:
+ *   out[i*out_stride + j] = T( scale * sum_k a[i][k] b[j][k] )
+ * Products are exact, sums fp32 on the matrix cores (in an order that depends
+ * on dim only).  out: device, out_stride >= n. */
+ps_status ps_mx4_product(int64_t m, int64_t n, int32_t dim, const uint8_t* a_codes, const uint8_t* a_scales,
+                         const uint8_t* b_codes, const uint8_t* b_scales, float scale, int32_t out_type, void* out,
+                         int64_t out_stride, void* stream);
+
+/* ======================================================================
  * Wide & Deep click-through-rate step (Appendix C, "Click-through-rate
  * prediction": the Wide & Deep model, AdaGrad).
  *

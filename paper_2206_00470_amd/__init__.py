@@ -8,12 +8,17 @@ and a missing library is an error, never a fallback.
 """
 import importlib
 
-__all__ = ["Store", "StagedStore", "dedup", "action_timing", "workloads"]
+_STORE = ("Store", "StagedStore", "dedup", "action_timing")
+_OPERATORS = ("ClipPlan", "MX4", "clip_grads", "grad_norm", "mx4_product", "mx4_quantize")
+
+__all__ = [*_STORE, *_OPERATORS, "workloads"]
 
 
 def __getattr__(name):
-    if name in ("Store", "StagedStore", "dedup", "action_timing"):
+    if name in _STORE:
         return getattr(importlib.import_module(__name__ + ".store"), name)
+    if name in _OPERATORS:
+        return getattr(importlib.import_module(__name__ + ".operators"), name)
     if name == "workloads":
         return importlib.import_module(__name__ + ".workloads")
     raise AttributeError(name)

@@ -32,6 +32,9 @@ PS_KERNEL_ASYNC = 7
 PS_TIMING_ALL = -1
 PS_PROBE_GRID = 2048
 
+PS_F32, PS_BF16, PS_F16 = 0, 1, 2
+PS_NO_PAD = -(1 << 63)
+
 STAGE_STATS = ["clock", "rounds", "forced", "staged", "evicted", "resident", "pending", "stalled", "plan_us"]
 
 _p, _i64, _i32, _f32, _sz = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
@@ -70,6 +73,16 @@ SIGNATURES = {
     "ps_probe_gather": (_i32, [_p, _p, _i64, _p, _p]),
     "ps_set_timing": (_i32, [_p, _i32]),
     "ps_read_timing": (_i32, [_p, _i32, C.POINTER(C.c_double), C.POINTER(_i64)]),
+    "ps_embed": (_i32, [_p, _p, _i64, _i64, _f32, _i32, _p, _i64, _p]),
+    "ps_embed_grad_workspace_bytes": (_sz, [_i32, _i64]),
+    "ps_embed_grad": (_i32, [_p, _p, _i64, _i64, _f32, _i32, _p, _i64, _i32, _p, _i64, _i32, _p, _sz, _p]),
+    "ps_embed_grad_rows": (_i32, [_p, _p, _i64, _i64, _f32, _i32, _p, _i64, _i32, _p, _p, _i64, _p, _p, _sz, _p]),
+    "ps_clip_workspace_bytes": (_sz, [_i32]),
+    "ps_grad_norm": (_i32, [_i32, _p, _p, _p, _p, _p, _sz, _p]),
+    "ps_clip_grads": (_i32, [_i32, _p, _p, _p, _p, C.c_double, _p, _p, _sz, _p]),
+    "ps_mx4_quantize": (_i32, [_i64, _i32, _i32, _p, _i64, _p, _p, _p]),
+    "ps_mx4_embed": (_i32, [_p, _p, _i64, _i32, _p, _i64, _i64, _f32, _i32, _p, _i64, _p, _p]),
+    "ps_mx4_product": (_i32, [_i64, _i64, _i32, _p, _p, _p, _p, _f32, _i32, _p, _i64, _p]),
     "ps_ctr_wd_workspace_bytes": (_sz, [_i64, _i32, _i64, _i32, _i32, _i32, _p]),
     "ps_step_ctr_wd": (_i32, [_p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p, _p, _p, _sz, _p]),
     "ps_create_staged": (_i32, [C.POINTER(_p), _i64, _i32, _p, _p, _i64, _p, _p, _i64, _p, _i32, _p, _p, _f32, _f32,

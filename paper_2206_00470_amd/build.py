@@ -12,13 +12,15 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libadapm_hip.so")
-SOURCES = [os.path.join(CSRC, "api.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("library.hip", "embed.hip", "clip.hip", "mx4.hip")]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -26,7 +28,6 @@ HIPCC_FLAGS = [
     "-O3",
     "-std=c++20",
     "-fPIC",
-    "-shared",
     "-ffp-contract=off",
     "-fhip-fp32-correctly-rounded-divide-sqrt",
     "-fno-gpu-flush-denormals-to-zero",
@@ -43,9 +44,7 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found: the HIP library cannot be built")
 
 
-def build(verbose: bool = False) -> str:
-    tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", INCLUDE, "-I", CSRC, "-o", tmp, *SOURCES]
+def _run(cmd, verbose: bool):
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -56,6 +55,17 @@ def build(verbose: bool = False) -> str:
         raise RuntimeError("hipcc failed:\n" + err)
     if verbose and err.strip():
         print(err, file=sys.stderr)
+
+
+def build(verbose: bool = False) -> str:
+    """Compile the sources side by side and link them."""
+    tmp = LIB + ".tmp%d" % os.getpid()
+    with tempfile.TemporaryDirectory() as work:
+        objects = [os.path.join(work, os.path.basename(src) + ".o") for src in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            list(pool.map(lambda so: _run([hipcc(), *HIPCC_FLAGS, "-I", INCLUDE, "-I", CSRC, "-c", "-o", so[1], so[0]],
+                                          verbose), zip(SOURCES, objects)))
+        _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-o", tmp, *objects], verbose)
     os.replace(tmp, LIB)
     return LIB
 

@@ -1,0 +1,236 @@
+// Entry points of the token table's lookup and of its gradient.
+#include "embed.hpp"
+
+#include <algorithm>
+#include <climits>
+
+#include "internal.hpp"
+#include "rules.hpp"
+
+using namespace adapm;
+
+namespace {
+
+ps_status check_type(int32_t type) {
+  if (type != PS_F32 && type != PS_BF16 && type != PS_F16) return raise(PS_ERR_INVALID, "unknown element type %d", type);
+  return PS_OK;
+}
+
+ps_status check_count(int64_t n) {
+  if (n < 0) return raise(PS_ERR_INVALID, "negative size %lld", (long long)n);
+  if (n > OCC_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld ids exceed the 32-bit occurrence index", (long long)n);
+  return PS_OK;
+}
+
+// Whether rows of elements of `bytes` bytes at p, ld apart, can be accessed
+// vw elements (at most 16 bytes of them) at a time.
+bool rows_vector(const void* p, int64_t ld, int bytes, int vw) {
+  return ld % vw == 0 && on_bytes(p, std::min(vw * bytes, 16));
+}
+
+template <class F>
+ps_status with_width(int vw, F&& f) {
+  if (vw == 8) return f.template operator()<8>();
+  if (vw == 4) return f.template operator()<4>();
+  return f.template operator()<1>();
+}
+
+}  // namespace
+
+extern "C" {
+
+ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t out_type, void* out,
+                   int64_t out_stride, void* stream) {
+  if (!s) return raise(PS_ERR_INVALID, "store is NULL");
+  if (ps_status r = check_count(n)) return r;
+  if (ps_status r = check_type(out_type)) return r;
+  const TableView t = table_view(s);
+  if (out_stride < t.dim) return raise(PS_ERR_INVALID, "out_stride %lld < dim %d", (long long)out_stride, t.dim);
+  if (n == 0) return PS_OK;
+  if (!ids || !out) return raise(PS_ERR_INVALID, "ids or out is NULL");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int vb = t.bf16 ? 2 : 4, ob = type_bytes(out_type);
+  if (!on_bytes(out, ob)) return raise(PS_ERR_INVALID, "out is not aligned to its elements");
+  auto fits = [&](int vw) {
+    return t.dim % vw == 0 && rows_vector(t.values, t.ld, vb, vw) && rows_vector(out, out_stride, ob, vw);
+  };
+  const int vw = fits(8) ? 8 : fits(4) ? 4 : 1;
+  const SmallDiv nv = small_div((uint32_t)(t.dim / vw));
+  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * EMBED_FLIGHT);
+  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the lookup's grid", (long long)n, t.dim);
+  const LookupIds l{ids, n, pad, t.num_keys, t.map, t.map_keys, t.status};
+  return with_type(out_type, [&]<class OT>(OT) -> ps_status {
+    return with_width(vw, [&]<int VW>() -> ps_status {
+      auto launch = [&](auto kernel, auto values) {
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, st, values, t.ld, l, nv, scale, static_cast<OT*>(out),
+                           out_stride);
+      };
+      if (t.bf16) launch(k_embed<bf16_t, OT, VW, false>, static_cast<const bf16_t*>(t.values));
+      else launch(k_embed<float, OT, VW, false>, static_cast<const float*>(t.values));
+      RAISE_HIP(hipGetLastError());
+      return PS_OK;
+    });
+  });
+}
+
+}  // extern "C"
+
+// ======================================================================== gradient
+namespace {
+
+struct GradPlan {
+  size_t order = 0;        // the sort's share, at the start
+  double* partial = nullptr;
+  double* fold = nullptr;
+  int32_t* split_list = nullptr;
+  uint32_t* split_count = nullptr;
+  size_t bytes = 0;
+};
+
+GradPlan plan_grad(void* ws, int64_t n, int dim) {
+  GradPlan p;
+  p.order = order_bytes(n);
+  size_t off = p.order;
+  auto take = [&](size_t bytes) {
+    off = (off + 255) & ~size_t(255);
+    char* q = ws ? static_cast<char*>(ws) + off : nullptr;
+    off += bytes;
+    return q;
+  };
+  const int64_t blocks = div_up(n, GRAD_BLOCK);
+  p.partial = reinterpret_cast<double*>(take(size_t(2) * blocks * dim * sizeof(double)));
+  p.fold = reinterpret_cast<double*>(take(size_t(blocks / GRAD_FOLD) * dim * sizeof(double)));
+  p.split_list = reinterpret_cast<int32_t*>(take(size_t(blocks) * sizeof(int32_t)));
+  p.split_count = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
+  p.bytes = off + 256;
+  return p;
+}
+
+struct GradCall {
+  const int64_t* ids;
+  int64_t n;
+  int64_t pad;
+  float scale;
+  int32_t in_type;
+  const void* dout;
+  int64_t in_ld;
+  GradOut out;
+  int64_t* uniq;         // rows form
+  int32_t* num_unique;   // rows form
+};
+
+ps_status clear_rows(const GradOut& o, int64_t rows, int dim, hipStream_t st) {
+  const int h = o.type == PS_F32 ? 2 : 1;   // 16-bit words per element
+  int64_t halves = int64_t(dim) * h, ld = o.ld * h;
+  if (ld == halves || rows == 1) {   // one stretch
+    halves *= rows;
+    rows = 1;
+    ld = halves;
+  }
+  const int vec = halves % 8 == 0 && ld % 8 == 0 && on_bytes(o.p, 16) ? 8
+                  : halves % 2 == 0 && ld % 2 == 0 && on_bytes(o.p, 4) ? 2 : 1;
+  const int64_t grid = std::min<int64_t>(div_up(rows * (halves / vec), BLOCK * 4), 8192);
+  hipLaunchKernelGGL(k_grad_clear, dim3(grid), dim3(BLOCK), 0, st, static_cast<uint16_t*>(o.p), rows, halves, ld, vec);
+  RAISE_HIP(hipGetLastError());
+  return PS_OK;
+}
+
+ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, hipStream_t st) {
+  if (!s) return raise(PS_ERR_INVALID, "store is NULL");
+  const TableView t = table_view(s);
+  if (t.map) return raise(PS_ERR_UNSUPPORTED, "the lookup's gradient is not available on a staged store");
+  if (ps_status r = check_count(c.n)) return r;
+  if (ps_status r = check_type(c.in_type)) return r;
+  if (ps_status r = check_type(c.out.type)) return r;
+  if (c.in_ld < t.dim || c.out.ld < t.dim) return raise(PS_ERR_INVALID, "a row stride is smaller than dim %d", t.dim);
+  if (!c.out.p) return raise(PS_ERR_INVALID, "grad is NULL");
+  const bool rows = c.num_unique != nullptr;
+  const int ib = type_bytes(c.in_type), ob = type_bytes(c.out.type);
+  if (!on_bytes(c.out.p, ob)) return raise(PS_ERR_INVALID, "grad is not aligned to its elements");
+  if (c.n == 0) {
+    if (rows) {
+      hipLaunchKernelGGL(k_grad_clear, dim3(1), dim3(BLOCK), 0, st, reinterpret_cast<uint16_t*>(c.num_unique),
+                         int64_t(1), int64_t(2), int64_t(2), 2);
+      RAISE_HIP(hipGetLastError());
+      return PS_OK;
+    }
+    return c.out.accumulate ? PS_OK : clear_rows(c.out, t.num_keys, t.dim, st);
+  }
+  if (!c.ids || !c.dout || (rows && !c.uniq)) return raise(PS_ERR_INVALID, "ids, dout or uniq is NULL");
+  if (!on_bytes(c.dout, ib)) return raise(PS_ERR_INVALID, "dout is not aligned to its elements");
+  const GradPlan p = plan_grad(ws, c.n, t.dim);
+  if (!ws) return raise(PS_ERR_INVALID, "workspace pointer is NULL");
+  if (ws_bytes < p.bytes) return raise(PS_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, p.bytes);
+  if (!on_bytes(ws, 16)) return raise(PS_ERR_INVALID, "the workspace must be 16-byte aligned");
+
+  auto fits = [&](int vw) {
+    return t.dim % vw == 0 && rows_vector(c.dout, c.in_ld, ib, vw) && rows_vector(c.out.p, c.out.ld, ob, vw);
+  };
+  const int vw = ib == 2 && fits(8) ? 8 : fits(4) ? 4 : 1;
+  const int vectors = t.dim / vw;
+  int lanes = 4;
+  while (lanes < WAVE && lanes < vectors) lanes *= 2;
+  const int slices = (int)div_up(vectors, lanes);
+  const int64_t blocks = div_up(c.n, GRAD_BLOCK);
+  const int64_t grid = div_up(blocks * slices, BLOCK / lanes);
+  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld ids of %d exceed the merge's grid", (long long)c.n, t.dim);
+
+  if (!rows && !c.out.accumulate)
+    if (ps_status r = clear_rows(c.out, t.num_keys, t.dim, st)) return r;
+  Order o;
+  if (ps_status r = order_ids(c.ids, c.n, c.pad, t.num_keys, ws, rows, c.uniq, p.split_count, t.status, st, &o))
+    return r;
+  const GradRuns g{o.keys, o.perm, c.n, (uint32_t)t.num_keys, rows ? o.seg_off : nullptr, o.hdr, c.num_unique,
+                   p.partial, p.split_list, p.split_count};
+  const ps_status r = with_type(c.in_type, [&]<class IT>(IT) -> ps_status {
+    return with_width(vw, [&]<int VW>() -> ps_status {
+      if constexpr (sizeof(IT) * VW <= 16) {
+        hipLaunchKernelGGL((k_grad_merge<IT, VW>), dim3(grid), dim3(BLOCK), 0, st, g, static_cast<const IT*>(c.dout),
+                           c.in_ld, t.dim, lanes, slices, (double)c.scale, c.out);
+        RAISE_HIP(hipGetLastError());
+      }
+      return PS_OK;
+    });
+  });
+  if (r) return r;
+  if (blocks < 2) return PS_OK;   // no run over several blocks
+  const int col_slices = (int)div_up(t.dim, WAVE);
+  const int64_t supers = blocks / GRAD_FOLD;
+  if (supers > 1) {   // (the first is never folded)
+    hipLaunchKernelGGL(k_grad_fold, dim3(std::min<int64_t>(supers * col_slices, 2048)), dim3(BLOCK), 0, st, g, supers,
+                       t.dim, col_slices, p.fold);
+    RAISE_HIP(hipGetLastError());
+  }
+  hipLaunchKernelGGL(k_grad_finish, dim3(std::min<int64_t>(blocks * col_slices, 2048)), dim3(BLOCK), 0, st, g, t.dim,
+                     col_slices, p.fold, (double)c.scale, c.out);
+  RAISE_HIP(hipGetLastError());
+  return PS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ps_embed_grad_workspace_bytes(int32_t dim, int64_t n) {
+  if (dim < 1 || n < 1 || n > OCC_MAX) return 0;
+  return plan_grad(nullptr, n, dim).bytes;
+}
+
+ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+                        const void* dout, int64_t dout_stride, int32_t out_type, void* grad, int64_t grad_stride,
+                        int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return embed_grad(s, GradCall{ids, n, pad, scale, in_type, dout, dout_stride,
+                                GradOut{grad, grad_stride, out_type, accumulate != 0}, nullptr, nullptr},
+                    ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+                             const void* dout, int64_t dout_stride, int32_t out_type, int64_t* uniq, void* rows,
+                             int64_t rows_stride, int32_t* num_unique, void* ws, size_t ws_bytes, void* stream) {
+  if (!num_unique) return raise(PS_ERR_INVALID, "num_unique is NULL");
+  return embed_grad(s, GradCall{ids, n, pad, scale, in_type, dout, dout_stride,
+                                GradOut{rows, rows_stride, out_type, 0}, uniq, num_unique},
+                    ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,125 @@
+// Entry points of the microscaled 4-bit tables.
+#include "mx4.hpp"
+
+#include <algorithm>
+#include <climits>
+
+#include "internal.hpp"
+
+using namespace adapm;
+
+namespace {
+
+constexpr int MX_DIM_MAX = 16384;
+
+ps_status check_dim(int32_t dim) {
+  if (dim < 1 || dim > MX_DIM_MAX) return raise(PS_ERR_UNSUPPORTED, "dim %d outside [1, %d]", dim, MX_DIM_MAX);
+  return PS_OK;
+}
+
+ps_status check_type(int32_t type) {
+  if (type != PS_F32 && type != PS_BF16 && type != PS_F16) return raise(PS_ERR_INVALID, "unknown element type %d", type);
+  return PS_OK;
+}
+
+int blocks_of(int dim) { return (dim + MX_BLOCK - 1) / MX_BLOCK; }
+
+}  // namespace
+
+extern "C" {
+
+ps_status ps_mx4_quantize(int64_t rows, int32_t dim, int32_t type, const void* x, int64_t row_stride, uint8_t* codes,
+                          uint8_t* scales, void* stream) {
+  if (rows < 0) return raise(PS_ERR_INVALID, "negative size %lld", (long long)rows);
+  if (ps_status r = check_dim(dim)) return r;
+  if (ps_status r = check_type(type)) return r;
+  if (row_stride < dim) return raise(PS_ERR_INVALID, "row_stride %lld < dim %d", (long long)row_stride, dim);
+  if (rows == 0) return PS_OK;
+  if (!x || !codes || !scales) return raise(PS_ERR_INVALID, "x, codes or scales is NULL");
+  const int b = type_bytes(type);
+  if (!on_bytes(x, b)) return raise(PS_ERR_INVALID, "x is not aligned to its elements");
+  if (!on_bytes(codes, 16)) return raise(PS_ERR_INVALID, "codes must be 16-byte aligned");
+  const SmallDiv per_row = small_div((uint32_t)blocks_of(dim) * 4);
+  if (rows > INT64_MAX / (4 * per_row.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)rows);
+  const int64_t grid = div_up(rows * per_row.d, int64_t(BLOCK) * QUANT_FLIGHT);
+  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)rows, dim);
+  const bool vec = dim % 8 == 0 && row_stride % 8 == 0 && on_bytes(x, 16);
+  return with_type(type, [&]<class T>(T) -> ps_status {
+    auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
+                         static_cast<const T*>(x), rows, dim, row_stride, per_row, reinterpret_cast<uint32_t*>(codes),
+                         scales);
+    };
+    if (vec) launch(k_mx4_quantize<T, true>);
+    else launch(k_mx4_quantize<T, false>);
+    RAISE_HIP(hipGetLastError());
+    return PS_OK;
+  });
+}
+
+ps_status ps_mx4_embed(const uint8_t* codes, const uint8_t* scales, int64_t num_rows, int32_t dim, const int64_t* ids,
+                       int64_t n, int64_t pad, float scale, int32_t out_type, void* out, int64_t out_stride,
+                       int32_t* err, void* stream) {
+  if (num_rows < 0) return raise(PS_ERR_INVALID, "negative size %lld", (long long)num_rows);
+  if (n < 0) return raise(PS_ERR_INVALID, "negative size %lld", (long long)n);
+  if (ps_status r = check_dim(dim)) return r;
+  if (ps_status r = check_type(out_type)) return r;
+  if (out_stride < dim) return raise(PS_ERR_INVALID, "out_stride %lld < dim %d", (long long)out_stride, dim);
+  if (!ids && n > num_rows) return raise(PS_ERR_INVALID, "%lld rows of a table of %lld", (long long)n, (long long)num_rows);
+  if (n == 0) return PS_OK;
+  if (!out || (num_rows > 0 && (!codes || !scales))) return raise(PS_ERR_INVALID, "codes, scales or out is NULL");
+  if (ids && !err) return raise(PS_ERR_INVALID, "err is NULL");
+  if (!on_bytes(codes, 16)) return raise(PS_ERR_INVALID, "codes must be 16-byte aligned");
+  const int b = type_bytes(out_type);
+  if (!on_bytes(out, b)) return raise(PS_ERR_INVALID, "out is not aligned to its elements");
+  auto fits = [&](int vw) { return dim % vw == 0 && out_stride % vw == 0 && on_bytes(out, std::min(vw * b, 16)); };
+  const int vw = fits(8) ? 8 : fits(4) ? 4 : 1;
+  const SmallDiv nv = small_div((uint32_t)((dim + 7) / 8));
+  if (n > INT64_MAX / (4 * nv.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)n);
+  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * EMBED_FLIGHT);
+  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)n, dim);
+  const LookupIds l{ids, n, pad, num_rows, nullptr, 0, err};
+  return with_type(out_type, [&]<class OT>(OT) -> ps_status {
+    auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
+                         reinterpret_cast<const uint32_t*>(codes), scales, blocks_of(dim), dim, l, nv, scale,
+                         static_cast<OT*>(out), out_stride);
+    };
+    if (vw == 8) launch(k_mx4_embed<OT, 8>);
+    else if (vw == 4) launch(k_mx4_embed<OT, 4>);
+    else launch(k_mx4_embed<OT, 1>);
+    RAISE_HIP(hipGetLastError());
+    return PS_OK;
+  });
+}
+
+ps_status ps_mx4_product(int64_t m, int64_t n, int32_t dim, const uint8_t* a_codes, const uint8_t* a_scales,
+                         const uint8_t* b_codes, const uint8_t* b_scales, float scale, int32_t out_type, void* out,
+                         int64_t out_stride, void* stream) {
+  if (m < 0 || n < 0) return raise(PS_ERR_INVALID, "negative size %lld x %lld", (long long)m, (long long)n);
+  if (ps_status r = check_dim(dim)) return r;
+  if (ps_status r = check_type(out_type)) return r;
+  if (out_stride < n) return raise(PS_ERR_INVALID, "out_stride %lld < %lld", (long long)out_stride, (long long)n);
+  if (m == 0 || n == 0) return PS_OK;
+  if (!a_codes || !a_scales || !b_codes || !b_scales || !out)
+    return raise(PS_ERR_INVALID, "codes, scales or out is NULL");
+  if (!on_bytes(a_codes, 16) || !on_bytes(b_codes, 16)) return raise(PS_ERR_INVALID, "codes must be 16-byte aligned");
+  if (!on_bytes(out, type_bytes(out_type))) return raise(PS_ERR_INVALID, "out is not aligned to its elements");
+  constexpr int64_t kRows = int64_t(1) << 40;
+  if (m > kRows || n > kRows) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld rows", (long long)m, (long long)n);
+  const MxRows A{a_codes, a_scales, m}, B{b_codes, b_scales, n};
+  return with_type(out_type, [&]<class OT>(OT) -> ps_status {
+    auto launch = [&](auto kernel, int tile_m, int tile_n) -> ps_status {
+      const int64_t tm = div_up(m, tile_m), tn = div_up(n, tile_n);
+      if (tm > INT_MAX / tn) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld exceed the grid", (long long)m, (long long)n);
+      hipLaunchKernelGGL(kernel, dim3(tm * tn), dim3(BLOCK), 0, static_cast<hipStream_t>(stream), A, B, blocks_of(dim),
+                         scale, static_cast<OT*>(out), out_stride, tn);
+      RAISE_HIP(hipGetLastError());
+      return PS_OK;
+    };
+    if (m <= 32) return launch(k_mx4_product<OT, 1, 1, 1, 4>, 32, 128);
+    return launch(k_mx4_product<OT, 2, 2, 2, 2>, 128, 128);
+  });
+}
+
+}  // extern "C"

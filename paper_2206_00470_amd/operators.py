@@ -1,0 +1,184 @@
+"""Operators on gradients and on quantised tables: the global gradient norm
+with clipping, and rows in microscaled 4-bit floating point.
+
+As in ``store``, only argument marshalling happens here; the computation runs
+in the HIP kernels of ``libadapm_hip.so``.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import _lib
+from ._lib import check, lib
+from .store import _dev, _On, _pad, _ptr, _rows, _type
+
+
+# ---------------------------------------------------------------------------- norm and clipping
+def _dense(t: torch.Tensor, device, name: str):
+    if not t.is_cuda or t.device != device:
+        raise TypeError(f"{name} must be CUDA tensors of one device")
+    if not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
+    return t
+
+
+class ClipPlan:
+    """The gradients of a model as one list, for its global norm and for
+    clipping by it: checked and marshalled once, for buffers that stay where
+    they are from step to step.  The plan keeps the tensors.
+
+    grads: contiguous CUDA tensors (float32, bfloat16, float16, mixed, of any
+    size) of one device.  out: where clipped gradients go, one tensor of the
+    same type and size for each (each its gradient itself, or apart from all
+    others); None: in place."""
+
+    def __init__(self, grads, out=None):
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        if len(out) != len(grads):
+            raise ValueError("out must have one tensor per gradient")
+        if not grads:
+            raise ValueError("need at least one gradient")
+        self.grads, self.out, self.device = grads, out, grads[0].device
+        for g, o in zip(grads, out):
+            _dense(g, self.device, "grads")
+            _dense(o, self.device, "out")
+            if o.dtype != g.dtype or o.shape != g.shape:
+                raise ValueError("an output must have its gradient's type and shape")
+        k = len(grads)
+        self._n = k
+        self._types = (C.c_int32 * k)(*(_type(g.dtype, "grads") for g in grads))
+        self._numel = (C.c_int64 * k)(*(g.numel() for g in grads))
+        self._in = (C.c_void_p * k)(*(g.data_ptr() for g in grads))
+        self._out = (C.c_void_p * k)(*(o.data_ptr() for o in out))
+        self._words = int(lib().ps_clip_workspace_bytes(k)) // 8
+
+    def _buffers(self):
+        # of its own per call: a captured call keeps the ones it was captured with
+        buf = torch.empty(1 + self._words, dtype=torch.float64, device=self.device)
+        return buf[:1], C.c_void_p(buf.data_ptr() + 8), 8 * self._words
+
+    def norm(self, stream=None) -> torch.Tensor:
+        """The global norm of the gradients, float64[1]."""
+        with _On(self.device, stream) as st:
+            norm, ws, wsb = self._buffers()
+            check(lib().ps_grad_norm(self._n, self._in, self._numel, self._types, _ptr(norm), ws, wsb, st))
+        return norm
+
+    def clip(self, max_norm: float, stream=None) -> torch.Tensor:
+        """Write the gradients, scaled by max_norm / norm where the norm is
+        larger, to the outputs; returns the norm before, float64[1]."""
+        with _On(self.device, stream) as st:
+            norm, ws, wsb = self._buffers()
+            check(lib().ps_clip_grads(self._n, self._in, self._out, self._numel, self._types, max_norm, _ptr(norm), ws,
+                                      wsb, st))
+        return norm
+
+
+def grad_norm(grads, stream=None) -> torch.Tensor:
+    """The global norm of a list of gradients, float64[1] (see ClipPlan)."""
+    return ClipPlan(grads).norm(stream)
+
+
+def clip_grads(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
+    """Clip a list of gradients by their global norm, in place or into out;
+    returns the norm before, float64[1] (see ClipPlan)."""
+    return ClipPlan(grads, out).clip(max_norm, stream)
+
+
+# ---------------------------------------------------------------------------- microscaled 4-bit rows
+MX_BLOCK = 32
+
+
+class MX4:
+    """Rows of dim values in microscaled 4-bit floating point: codes
+    uint8[rows, ceil(dim/32)*16] (two to a byte, the first in the low half) and
+    scales uint8[rows, ceil(dim/32)], contiguous CUDA tensors.  A read-only
+    copy of a table at 4.25 bits a value; see mx4_quantize."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, dim: int):
+        _dev(codes, torch.uint8, "codes")
+        _dev(scales, torch.uint8, "scales")
+        nb = -(-dim // MX_BLOCK)
+        if codes.dim() != 2 or scales.dim() != 2 or dim < 1:
+            raise ValueError("codes and scales must be [rows, ...] and dim at least 1")
+        if codes.shape[0] != scales.shape[0] or scales.shape[1] != nb or codes.shape[1] != 16 * nb:
+            raise ValueError(f"rows of {dim} values have {16 * nb} bytes of codes and {nb} scales")
+        if codes.device != scales.device:
+            raise TypeError("codes and scales must be on one device")
+        self.codes, self.scales, self.dim = codes, scales, dim
+        self.rows, self.device = codes.shape[0], codes.device
+        self._err = None
+
+    def embed(self, ids: torch.Tensor, scale: float = 1.0, dtype: torch.dtype = torch.float32, pad: int | None = None,
+              out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """Store.embed from these rows; an id outside them gives zeros and
+        raises the sticky error that error() reports."""
+        _dev(ids, torch.int64, "ids")
+        if ids.device != self.device:
+            raise TypeError(f"ids must be on {self.device}")
+        return self._lookup(ids, ids.numel(), ids.shape, scale, dtype, pad, out, stream)
+
+    def dequantize(self, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None,
+                   stream=None) -> torch.Tensor:
+        """The values of all rows, [rows, dim] of dtype."""
+        return self._lookup(None, self.rows, (self.rows,), 1.0, dtype, None, out, stream)
+
+    def _lookup(self, ids, n, shape, scale, dtype, pad, out, stream):
+        with _On(self.device, stream) as st:
+            if ids is not None and self._err is None:
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("the first embed of a table makes its error flag: call it before a capture")
+                self._err = torch.zeros(2, dtype=torch.int32, device=self.device)
+            if out is None:
+                out = torch.empty((*shape, self.dim), dtype=dtype, device=self.device)
+            rows, ld = _rows(out, self.dim, self.device, "out")
+            if rows != n:
+                raise ValueError("out must have one row per id")
+            check(lib().ps_mx4_embed(_ptr(self.codes), _ptr(self.scales), self.rows, self.dim, _ptr(ids), n, _pad(pad),
+                                     scale, _type(out.dtype, "out"), _ptr(out), ld,
+                                     _ptr(self._err if ids is not None else None), st))
+        return out
+
+    def error(self) -> int:
+        """Synchronize, then return and clear the sticky status of embed."""
+        if self._err is None or not int(self._err[0].item()):
+            return _lib.PS_OK
+        self._err.zero_()
+        return _lib.PS_ERR_KEY_RANGE
+
+
+def mx4_quantize(x: torch.Tensor, stream=None) -> MX4:
+    """Quantise the rows of x ([rows, dim], float32, bfloat16 or float16, unit
+    column stride; a store's value table W as it is)."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, dim]")
+    rows, dim = x.shape
+    _, ld = _rows(x, dim, x.device, "x")
+    nb = -(-dim // MX_BLOCK)
+    with _On(x.device, stream) as st:
+        codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=x.device)
+        scales = torch.empty((rows, nb), dtype=torch.uint8, device=x.device)
+        check(lib().ps_mx4_quantize(rows, dim, _type(x.dtype, "x"), _ptr(x), ld, _ptr(codes), _ptr(scales), st))
+    return MX4(codes, scales, dim)
+
+
+def mx4_product(a: MX4, b: MX4, scale: float = 1.0, dtype: torch.dtype = torch.float32,
+                out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Scores of quantised queries against quantised rows, scale * a b^T as
+    [a.rows, b.rows] of dtype."""
+    if a.dim != b.dim:
+        raise ValueError(f"rows of {a.dim} and of {b.dim} values")
+    if a.device != b.device:
+        raise TypeError("the operands must be on one device")
+    with _On(a.device, stream) as st:
+        if out is None:
+            out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
+        if tuple(out.shape) != (a.rows, b.rows):
+            raise ValueError(f"out must be [{a.rows}, {b.rows}]")
+        _, ld = _rows(out, b.rows, a.device, "out")
+        check(lib().ps_mx4_product(a.rows, b.rows, a.dim, _ptr(a.codes), _ptr(a.scales), _ptr(b.codes),
+                                   _ptr(b.scales), scale, _type(out.dtype, "out"), _ptr(out), ld, st))
+    return out

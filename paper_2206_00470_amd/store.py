@@ -30,6 +30,59 @@ def _dev(t: torch.Tensor, dtype, name: str):
     return t
 
 
+TYPES = {torch.float32: _lib.PS_F32, torch.bfloat16: _lib.PS_BF16, torch.float16: _lib.PS_F16}
+
+
+def _type(dtype, name: str) -> int:
+    if dtype not in TYPES:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, not {dtype}")
+    return TYPES[dtype]
+
+
+def _pad(pad) -> int:
+    return _lib.PS_NO_PAD if pad is None else int(pad)
+
+
+def _rows(t: torch.Tensor, cols: int, device, name: str):
+    """(row count, row stride) of a CUDA tensor [..., cols] of equidistant rows with unit column stride."""
+    if not t.is_cuda or t.device != device:
+        raise TypeError(f"{name} must be a CUDA tensor on {device}")
+    if t.dim() == 0 or t.shape[-1] != cols:
+        raise ValueError(f"{name} must have rows of {cols} elements")
+    n = t.numel() // cols if cols else 0
+    if t.is_contiguous() or n <= 1:
+        if n == 1 and cols > 1 and t.stride(-1) != 1:
+            raise TypeError(f"{name} must have unit column stride")
+        return n, cols
+    lead = [(s, st) for s, st in zip(t.shape[:-1], t.stride()[:-1]) if s != 1]
+    if cols > 1 and t.stride(-1) != 1:
+        raise TypeError(f"{name} must have unit column stride")
+    for (_, outer), (size, inner) in zip(lead, lead[1:]):
+        if outer != size * inner:
+            raise TypeError(f"the rows of {name} must be equidistant")
+    return n, lead[-1][1]
+
+
+class _On:
+    """The device of a call's tensors made current, and the stream of the call
+    (the device's current one if none is given) the one that new tensors
+    belong to."""
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.inner = device, stream, None
+        if stream is not None or torch.cuda.current_device() != device.index:
+            self.inner = torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device))
+
+    def __enter__(self):
+        if self.inner is not None:
+            self.inner.__enter__()
+        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def __exit__(self, *a):
+        if self.inner is not None:
+            self.inner.__exit__(*a)
+
+
 class Workspace:
     """A device byte buffer that grows to the largest request seen."""
 
@@ -223,6 +276,76 @@ class Store:
         if grads.numel() != n * self.dim:
             raise ValueError("grads must hold n*dim floats")
         check(lib().ps_push_async(self._h, _ptr(keys), n, _ptr(grads), _stream(stream)))
+
+    # ---------------------------------------------------------------- token table
+    def _ids(self, ids):
+        _dev(ids, torch.int64, "ids")
+        if ids.device != self.W.device:
+            raise TypeError(f"ids must be on {self.W.device}")
+        return ids.numel()
+
+    def embed(self, ids: torch.Tensor, scale: float = 1.0, dtype: torch.dtype = torch.float32, pad: int | None = None,
+              out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """Lookup with scaling: scale * W[ids] as ids.shape + (dim,) of dtype
+        (float32, bfloat16, float16); rows of zeros where ids == pad.  An id
+        outside the table gives zeros and raises the sticky error.  out:
+        equidistant rows, in place of a new tensor (dtype is then its own)."""
+        n = self._ids(ids)
+        with _On(self.W.device, stream) as st:
+            if out is None:
+                out = torch.empty((*ids.shape, self.dim), dtype=dtype, device=self.W.device)
+            rows, ld = _rows(out, self.dim, self.W.device, "out")
+            if rows != n:
+                raise ValueError("out must have one row per id")
+            check(lib().ps_embed(self._h, _ptr(ids), n, _pad(pad), scale, _type(out.dtype, "out"), _ptr(out), ld, st))
+        return out
+
+    def _grad_args(self, ids, dout):
+        n = self._ids(ids)
+        rows, ld = _rows(dout, self.dim, self.W.device, "dout")
+        if rows != n:
+            raise ValueError("dout must have one row per id")
+        nbytes = int(lib().ps_embed_grad_workspace_bytes(self.dim, n)) if n else 0
+        # a workspace of its own per call: a captured call keeps the one it was captured with
+        return n, ld, _type(dout.dtype, "dout"), torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.W.device)
+
+    def embed_grad(self, ids: torch.Tensor, dout: torch.Tensor, scale: float = 1.0, pad: int | None = None,
+                   dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, accumulate: bool = False,
+                   stream=None) -> torch.Tensor:
+        """Gradient of embed as a dense [num_keys, dim] tensor: row v holds
+        scale times the sum of dout's rows whose id is v.  out: the tensor to
+        write (its rows without an id become zero) or, with accumulate, to add
+        to."""
+        if accumulate and out is None:
+            raise ValueError("accumulate needs the gradient to add to (out)")
+        with _On(self.W.device, stream) as st:
+            n, ld, kind, ws = self._grad_args(ids, dout)
+            if out is None:
+                out = torch.empty((self.num_keys, self.dim), dtype=dtype, device=self.W.device)
+            rows, out_ld = _rows(out, self.dim, self.W.device, "out")
+            if rows != self.num_keys:
+                raise ValueError("out must have one row per key")
+            check(lib().ps_embed_grad(self._h, _ptr(ids), n, _pad(pad), scale, kind, _ptr(dout), ld,
+                                      _type(out.dtype, "out"), _ptr(out), out_ld, int(accumulate), _ptr(ws), ws.numel(),
+                                      st))
+        return out
+
+    def embed_grad_rows(self, ids: torch.Tensor, dout: torch.Tensor, scale: float = 1.0, pad: int | None = None,
+                        dtype: torch.dtype = torch.float32, stream=None):
+        """The same gradient as merged rows: (uniq, rows), the distinct ids in
+        ascending order and their gradient rows, as push takes them.  Waits
+        for the number of distinct ids."""
+        with _On(self.W.device, stream) as st:
+            n, ld, kind, ws = self._grad_args(ids, dout)
+            uniq = torch.empty(n, dtype=torch.int64, device=self.W.device)
+            rows = torch.empty((n, self.dim), dtype=dtype, device=self.W.device)
+            # (an address even where there are no ids)
+            count = torch.empty(1, dtype=torch.int32, device=self.W.device)
+            check(lib().ps_embed_grad_rows(self._h, _ptr(ids), n, _pad(pad), scale, kind, _ptr(dout), ld,
+                                           _type(dtype, "dtype"), _ptr(uniq), _ptr(rows) if n else _ptr(count),
+                                           self.dim, _ptr(count), _ptr(ws), ws.numel(), st))
+            U = int(count.item())
+        return uniq[:U], rows[:U]
 
     # ---------------------------------------------------------------- task steps
     def _loss(self, loss):

@@ -1,0 +1,390 @@
+"""The token table's lookup and its gradient against plain forms in 64 bits:
+every store layout and element type, odd widths and counts, strides, padding,
+hot ids, the two forms of the gradient and accumulation."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2206_00470_amd import StagedStore, Store, _lib
+from paper_2206_00470_amd._lib import PSError
+from paper_2206_00470_amd.store import interleaved_bf16_tables, interleaved_tables, padded_rowwise_table
+from tests.helpers import say
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+HALF = {t: torch.finfo(t).eps / 2 for t in (F32, BF16, F16)}   # of a rounding, relative
+TINY = {t: torch.finfo(t).smallest_normal * torch.finfo(t).eps / 2 for t in (F32, BF16, F16)}   # half a subnormal step
+
+
+def table(K, d, seed, dtype=F32):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn((K, d), generator=g).to(dtype)
+
+
+def make_store(layout, K, d, seed=1):
+    W = table(K, d, seed).cuda()
+    if layout == "dense":
+        return Store(W, torch.ones_like(W))
+    if layout == "interleaved":
+        return Store(*interleaved_tables(W))
+    if layout == "rowwise":
+        return Store(*padded_rowwise_table(W))
+    return Store(*interleaved_bf16_tables(W))
+
+
+def make_ids(K, n, seed, kind="zipf"):
+    rng = np.random.default_rng(seed)
+    if kind == "same":
+        ids = np.full(n, K - 1)
+    elif kind == "uniform":
+        ids = rng.integers(0, K, n)
+    else:
+        ids = (np.floor(K ** rng.random(n)).astype(np.int64) - 1) * 7919 % K
+    return torch.from_numpy(ids.astype(np.int64))
+
+
+def bits(t):
+    return t.contiguous().cpu().view(torch.int32 if t.dtype == F32 else torch.int16).numpy()
+
+
+# ------------------------------------------------------------------ lookup
+def plain_embed(W, ids, scale, dtype, pad):
+    ok = (ids >= 0) & (ids < W.shape[0])
+    if pad is not None:
+        ok &= ids != pad
+    rows = W.float()[torch.where(ok, ids, 0)] * torch.tensor(scale, dtype=F32)
+    return torch.where(ok[..., None], rows, torch.zeros(())).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("layout,d", [("dense", 1), ("dense", 3), ("dense", 33), ("dense", 100), ("dense", 512),
+                                      ("dense", 516), ("dense", 2048), ("dense", 16384), ("interleaved", 20),
+                                      ("interleaved", 300), ("rowwise", 36), ("rowwise", 65), ("bf16", 8), ("bf16", 101),
+                                      ("bf16", 300), ("bf16", 512)])
+def test_embed_is_the_rounded_product(layout, d, dtype):
+    K = 700 if d < 4096 else 40
+    s = make_store(layout, K, d)
+    W = s.W.cpu()
+    for n, pad in ((1, None), (2, 5), (257, 5), (1023, None), (4099 if d < 4096 else 99, -1)):
+        ids = make_ids(K, n, 10 + n)
+        if pad is not None:
+            ids[::3] = pad
+        say(f"embed {layout} d={d} n={n} {dtype}")
+        got = s.embed(ids.cuda(), scale=d ** 0.5, dtype=dtype, pad=pad)
+        assert got.shape == (n, d) and got.dtype == dtype
+        assert np.array_equal(bits(got), bits(plain_embed(W, ids, d ** 0.5, dtype, pad)))
+    assert s.error() == 0
+
+
+def test_embed_shapes_strides_and_errors():
+    K, d = 300, 48
+    s = make_store("dense", K, d)
+    W = s.W.cpu()
+    ids = make_ids(K, 60, 3).view(3, 4, 5)
+    assert s.embed(ids.cuda()).shape == (3, 4, 5, d)
+    # outputs inside a wider tensor: vectors, half vectors, single elements; neighbours untouched
+    for pitch, off in ((64, 8), (60, 4), (51, 1), (57, 0)):
+        wide = torch.full((60, pitch), 7.0, dtype=BF16, device="cuda")
+        out = wide[:, off:off + d]
+        got = s.embed(ids.cuda().view(60), scale=0.5, out=out)
+        assert got.data_ptr() == out.data_ptr()
+        assert np.array_equal(bits(out), bits(plain_embed(W, ids.view(60), 0.5, BF16, None)))
+        wide[:, off:off + d] = 7.0
+        assert bool((wide == 7.0).all())
+    # ids outside the table: zeros, the sticky error, and the others as ever
+    bad = torch.tensor([0, -1, K, K - 1, 2 ** 40, -2 ** 63 + 1], device="cuda")
+    got = s.embed(bad).cpu()
+    assert s.error() == _lib.PS_ERR_KEY_RANGE and s.error() == 0
+    assert bool((got[[1, 2, 4, 5]] == 0).all()) and torch.equal(got[0], W[0]) and torch.equal(got[3], W[K - 1])
+    # the same ids as padding are no error
+    s.embed(torch.tensor([0, -1, -1], device="cuda"), pad=-1)
+    s.embed(torch.tensor([0, K + 3], device="cuda"), pad=K + 3)
+    assert s.error() == 0
+    assert s.embed(ids[:0].cuda()).shape == (0, 4, 5, d)
+
+
+def test_embed_special_values_pass_through():
+    W = torch.tensor([[float("inf"), -float("inf"), float("nan"), 3.0e38, 1e-45, -0.0, 65520.0, 65519.0]]).cuda()
+    s = Store(W, torch.ones_like(W))
+    ids = torch.zeros(1, dtype=torch.int64, device="cuda")
+    for dtype in (F32, BF16, F16):
+        got, ref = s.embed(ids, dtype=dtype).cpu(), W.cpu().to(dtype)
+        assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got[~got.isnan()], ref[~ref.isnan()])
+        got = s.embed(ids, scale=2.0, dtype=dtype).cpu()
+        ref = (W.cpu() * 2.0).to(dtype)
+        assert torch.equal(got[~got.isnan()], ref[~ref.isnan()])
+        assert bool((s.embed(ids, scale=float("inf"), pad=0, dtype=dtype) == 0).all())   # padding stays zero
+
+
+def test_embed_offsets_beyond_32_bits():
+    """Rows and outputs whose element offsets pass 2^31 and 2^32."""
+    K, d = 9_000_000, 512
+    W = torch.empty((K, d), dtype=F32, device="cuda")
+    for at in (0, 4_194_303, 4_194_304, 8_388_608, K - 1):
+        W[at] = torch.arange(d, device="cuda", dtype=F32) + at % 1000
+    s = Store(W, torch.ones(K, device="cuda"))   # row-wise: one accumulator per key
+    ids = torch.tensor([0, 4_194_303, 4_194_304, 8_388_608, K - 1], device="cuda")
+    assert torch.equal(s.embed(ids), W[ids])
+    many = ids.repeat(1_000_000)[: 4_600_000]    # 2.4e9 output elements
+    out = s.embed(many, dtype=BF16)
+    for i in (0, 4_194_302, 4_194_304, 4_599_999):
+        assert torch.equal(out[i], W[many[i]].to(BF16)), i
+    assert s.error() == 0
+
+
+def test_embed_staged_store():
+    K, d = 400, 32
+    W0 = table(K, d, 9).numpy()
+    s = StagedStore(W0, [0], [200])
+    s.intent(np.arange(0, 200), 1, 5)
+    s.round(wait=True)
+    s.advance_clock()
+    ids = torch.randint(0, 200, (1000,), device="cuda")
+    got = s.embed(ids, scale=2.0, dtype=BF16)
+    assert s.error() == 0
+    assert np.array_equal(bits(got), bits(plain_embed(torch.from_numpy(W0), ids.cpu(), 2.0, BF16, None)))
+    got = s.embed(torch.tensor([3, 250], device="cuda"))
+    assert s.error() == _lib.PS_ERR_NOT_RESIDENT and bool((got[1] == 0).all())
+    with pytest.raises(PSError) as e:
+        s.embed_grad_rows(ids, torch.zeros((1000, d), device="cuda"))
+    assert e.value.status == _lib.PS_ERR_UNSUPPORTED
+
+
+# ------------------------------------------------------------------ gradient
+def plain_grad(K, ids, dout, scale, pad):
+    """(sums in 64 bits, sums of magnitudes, counts), [K, d] and [K]."""
+    ok = (ids >= 0) & (ids < K)
+    if pad is not None:
+        ok &= ids != pad
+    d = dout.double()[ok]
+    s = torch.zeros((K, dout.shape[1]), dtype=torch.float64)
+    a = torch.zeros_like(s)
+    s.index_add_(0, ids[ok], d)
+    a.index_add_(0, ids[ok], d.abs())
+    return s * scale, a * abs(scale), torch.bincount(ids[ok], minlength=K)
+
+
+def check_grad(got, ref, mag, count, dtype, extra=0.0):
+    """Both sums in 64 bits: each off by at most count * 2^-53 of the sum of
+    magnitudes, and the kernel's product with scale by 2^-53 of the value; then
+    one rounding to fp32 and one to dtype."""
+    got = got.double().cpu()
+    c = count.double()[:, None] + 2
+    tol = 2 * c * 2.0 ** -53 * mag + (2.0 ** -24 + HALF[dtype]) * (1 + 2.0 ** -8) * (ref.abs() + extra) + 2 * TINY[dtype]
+    bad = ((got - ref).abs() > tol).sum()
+    assert int(bad) == 0, f"{int(bad)} of {got.numel()} off"
+
+
+GRADS = [  # K, d, n, ids
+    (50, 1, 1, "uniform"), (50, 3, 40, "zipf"), (1000, 20, 31, "uniform"), (1000, 33, 32, "same"), (1000, 64, 33, "same"),
+    (9, 100, 1000, "uniform"), (70_001, 100, 9001, "zipf"), (5000, 300, 2100, "zipf"), (64, 512, 4097, "zipf"),
+    (700, 516, 3000, "zipf"), (333, 1024, 5000, "zipf"), (40, 2052, 700, "same"), (40, 4096, 300, "zipf"),
+    (100, 16, 70_000, "same"), (3, 8, 400_003, "uniform"), (2_000_000, 12, 200_000, "zipf"), (17, 60, 4097, "same"),
+]
+
+
+@pytest.mark.parametrize("form", ["dense", "rows"])
+@pytest.mark.parametrize("K,d,n,kind", GRADS)
+def test_embed_grad_matches_sums_in_64_bits(K, d, n, kind, form):
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    ids = make_ids(K, n, 20 + d, kind)
+    pad = None
+    if n > 100 and kind == "zipf":
+        pad = int(ids[7])
+        ids[5::4] = pad
+    g = torch.Generator().manual_seed(30 + d)
+    for gin, gout in ((F32, F32), (BF16, F32), (F16, BF16), (BF16, BF16), (F32, F16)):
+        dout = torch.randn((n, d), generator=g).to(gin)
+        say(f"grad {form} K={K} d={d} n={n} {kind} {gin} -> {gout}")
+        ref, mag, count = plain_grad(K, ids, dout, 1.7, pad)
+        scale = float(torch.tensor(1.7, dtype=F32))   # what the call gets
+        ref, mag = ref * (scale / 1.7), mag * (scale / 1.7)
+        if form == "dense":
+            out = torch.full((K, d), 9.0, dtype=gout, device="cuda")
+            got = s.embed_grad(ids.cuda(), dout.cuda(), scale=1.7, pad=pad, out=out)
+            assert got is out
+            check_grad(got, ref, mag, count, gout)
+            assert bool((got.cpu()[count == 0] == 0).all())
+        else:
+            uniq, rows = s.embed_grad_rows(ids.cuda(), dout.cuda(), scale=1.7, pad=pad, dtype=gout)
+            want = torch.nonzero(count)[:, 0]
+            assert torch.equal(uniq.cpu(), want) and rows.dtype == gout
+            check_grad(rows, ref[want], mag[want], count[want], gout)
+    assert s.error() == 0
+    assert not W.cpu().numpy().any()
+
+
+@pytest.mark.parametrize("gout", [F32, BF16])
+@pytest.mark.parametrize("K,d,n,kind", [(50, 3, 40, "zipf"), (3000, 100, 5000, "zipf"), (64, 768, 4097, "same")])
+def test_embed_grad_accumulates(K, d, n, kind, gout):
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    ids = make_ids(K, n, 40, kind)
+    dout = torch.randn((n, d), generator=torch.Generator().manual_seed(41)).to(BF16)
+    old = torch.randn((K, d), generator=torch.Generator().manual_seed(42)).to(gout)
+    ref, mag, count = plain_grad(K, ids, dout, 1.0, None)
+    out = old.clone().cuda()
+    s.embed_grad(ids.cuda(), dout.cuda(), out=out, accumulate=True)
+    some = count > 0
+    check_grad(out.cpu()[some], ref[some] + old.double()[some], mag[some] + old.double()[some].abs(), count[some] + 1, gout)
+    assert np.array_equal(bits(out.cpu()[~some]), bits(old[~some]))
+
+
+def test_embed_grad_strides_errors_and_rows_left_alone():
+    K, d, n = 200, 40, 777
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    ids = make_ids(K, n, 50)
+    ref_ids = ids.clone()
+    ids[[3, 10, 600]] = torch.tensor([-7, K, 2 ** 50])
+    dout = torch.randn((n, d), generator=torch.Generator().manual_seed(51))
+    ref, mag, count = plain_grad(K, ids, dout, 1.0, None)
+    for pitch, off in ((48, 8), (44, 4), (45, 1), (53, 0)):
+        for gin in (F32, BF16):
+            wide = torch.zeros((n, pitch), dtype=gin, device="cuda")
+            wide[:, off:off + d] = dout.to(gin).cuda()
+            r, m, c = plain_grad(K, ids, dout.to(gin), 1.0, None)
+            big = torch.full((K, pitch), 5.0, device="cuda")
+            out = big[:, off:off + d]
+            s.embed_grad(ids.cuda(), wide[:, off:off + d], out=out)
+            assert s.error() == _lib.PS_ERR_KEY_RANGE
+            check_grad(out, r, m, c, F32)
+            big[:, off:off + d] = 5.0
+            assert bool((big == 5.0).all())
+    # [B, T, d] gradients, and the raw call: what lies behind the last row stays
+    got = s.embed_grad(ref_ids.cuda().view(7, 111), dout.cuda().view(7, 111, d))
+    check_grad(got, *plain_grad(K, ref_ids, dout, 1.0, None), F32)
+    L, p = _lib.lib(), lambda t: t.data_ptr()
+    uniq = torch.full((n,), -3, dtype=torch.int64, device="cuda")
+    rows = torch.full((n, d), 4.0, device="cuda")
+    num = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(L.ps_embed_grad_workspace_bytes(d, n), dtype=torch.uint8, device="cuda")
+    dev_ids, dev_dout = ids.cuda(), dout.cuda()
+    st = torch.cuda.current_stream().cuda_stream
+    args = lambda nb: (s._h, p(dev_ids), n, _lib.PS_NO_PAD, 1.0, 0, p(dev_dout), d, 0, p(uniq), p(rows), d, p(num), p(ws),
+                       nb, st)
+    assert L.ps_embed_grad_rows(*args(ws.numel() - 1)) == _lib.PS_ERR_WORKSPACE
+    assert L.ps_embed_grad_rows(*args(ws.numel())) == 0
+    U = int(num.item())
+    assert U == int((count > 0).sum())
+    assert bool((uniq[U:] == -3).all()) and bool((rows[U:] == 4.0).all())
+    check_grad(rows[:U], ref[count > 0], mag[count > 0], count[count > 0], F32)
+    assert s.error() == _lib.PS_ERR_KEY_RANGE
+
+
+def test_embed_grad_of_nothing():
+    K, d = 30, 12
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    none, rows0 = torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty((0, d), device="cuda")
+    out = torch.ones((K, d), device="cuda")
+    assert bool((s.embed_grad(none, rows0, out=out) == 0).all())
+    out.fill_(2.0)
+    s.embed_grad(none, rows0, out=out, accumulate=True)
+    assert bool((out == 2).all())
+    u, r = s.embed_grad_rows(none, rows0)
+    assert u.numel() == 0 and r.shape == (0, d)
+    pads = torch.full((70,), 4, dtype=torch.int64, device="cuda")
+    dout = torch.full((70, d), float("nan"), device="cuda")     # padded rows are not read into any sum
+    assert bool((s.embed_grad(pads, dout, pad=4, out=out) == 0).all())
+    u, r = s.embed_grad_rows(pads, dout, pad=4)
+    assert u.numel() == 0
+    assert s.error() == 0
+    with pytest.raises(ValueError):
+        s.embed_grad(pads, dout, accumulate=True)
+    with pytest.raises(ValueError):
+        s.embed_grad(pads, dout[:69])
+    with pytest.raises(TypeError):
+        s.embed_grad(pads, dout.double())
+    with pytest.raises(TypeError):
+        s.embed_grad(pads.int(), dout)
+    with pytest.raises(TypeError):
+        s.embed(pads, dtype=torch.float64)
+    with pytest.raises(TypeError):
+        s.embed(pads, out=torch.empty((70, 2 * d), device="cuda")[:, ::2])
+
+
+def test_embed_grad_special_values_and_same_bits():
+    K, d, n = 40, 64, 5000
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    ids = make_ids(K, n, 60)
+    dout = torch.randn((n, d), generator=torch.Generator().manual_seed(61))
+    hot = torch.nonzero(ids == ids[0])[:, 0]
+    dout[hot[0], 3], dout[hot[1], 4], dout[hot[2], 4], dout[hot[3], 5] = float("inf"), float("inf"), -float("inf"), float("nan")
+    a = s.embed_grad(ids.cuda(), dout.cuda())
+    row = a[int(ids[0])].cpu()
+    assert row[3] == float("inf") and row[4].isnan() and row[5].isnan() and bool(row[6:].isfinite().all())
+    for _ in range(3):
+        assert np.array_equal(bits(s.embed_grad(ids.cuda(), dout.cuda())), bits(a))
+
+
+def test_embed_grad_is_the_derivative_of_embed():
+    """Differences of a loss over the lookup: <dout, embed(W)> is linear in W,
+    so its difference quotients are the gradient but for fp32 rounding."""
+    K, d, n = 23, 20, 90
+    W = table(K, d, 70).cuda()
+    s = Store(W, torch.ones_like(W))
+    ids = make_ids(K, n, 71).cuda()
+    ids[::5] = 2
+    dout = torch.randn((n, d), generator=torch.Generator().manual_seed(72)).cuda()
+    grad = s.embed_grad(ids, dout, scale=1.5, pad=2).cpu()
+    loss = lambda: float((dout.double() * s.embed(ids, scale=1.5, pad=2).double()).sum())
+    base = loss()
+    for v, c in ((0, 0), (2, 3), (5, 7), (int(ids[1]), 19), (22, 11)):
+        keep = float(W[v, c])
+        h = float(torch.tensor(keep + 2.0) - torch.tensor(keep))   # exact in fp32
+        W[v, c] = keep + 2.0
+        diff = (loss() - base) / h
+        W[v, c] = keep
+        m = float(dout[ids == v].abs().sum()) * 1.5 + 1
+        # each looked-up product is off by 2^-24 of at most 1.5 * (|w| + 2)
+        assert abs(diff - float(grad[v, c])) <= 2.0 ** -23 * m * (abs(keep) + 3), (v, c)
+
+
+def test_lookup_and_gradient_in_graphs():
+    """Captured lookups and gradients of two graphs, replayed in turn beside
+    eager calls of the same store, which grow its workspaces."""
+    K, d = 900, 72
+    W = table(K, d, 80).cuda()
+    s = Store(W, torch.ones_like(W))
+    g = torch.Generator().manual_seed(81)
+    graphs = []
+    for n in (1500, 300):
+        ids, dout = make_ids(K, n, 82 + n).cuda(), torch.randn((n, d), generator=g).cuda()
+        out, grad = torch.empty((n, d), dtype=BF16, device="cuda"), torch.empty((K, d), device="cuda")
+        s.embed(ids, out=out), s.embed_grad(ids, dout, out=grad, pad=3)
+        torch.cuda.synchronize()
+        G = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(G):
+            s.embed(ids, scale=3.0, out=out)
+            s.embed_grad(ids, dout, out=grad, pad=3)
+        graphs.append((G, ids, dout, out, grad))
+    for r in range(4):
+        for G, ids, dout, out, grad in graphs:
+            ids.copy_(make_ids(K, ids.numel(), 90 + r))
+            dout.normal_()
+            out.fill_(5.0), grad.fill_(5.0)
+            G.replay()
+            big = make_ids(K, 20_000, 95 + r).cuda()
+            s.embed_grad(big, torch.ones((20_000, d), device="cuda"))
+            torch.cuda.synchronize()
+            assert np.array_equal(bits(out), bits(s.embed(ids, scale=3.0, dtype=BF16)))
+            assert np.array_equal(bits(grad), bits(s.embed_grad(ids, dout, pad=3)))
+    assert s.error() == 0
+
+
+def test_lookup_and_gradient_on_another_stream():
+    K, d, n = 5000, 64, 40_000
+    W = table(K, d, 85).cuda()
+    s = Store(W, torch.ones_like(W))
+    ids, dout = make_ids(K, n, 86).cuda(), torch.randn((n, d)).cuda()
+    a, b, (u, r) = s.embed(ids), s.embed_grad(ids, dout), s.embed_grad_rows(ids, dout)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    a2, b2, (u2, r2) = s.embed(ids, stream=side), s.embed_grad(ids, dout, stream=side), s.embed_grad_rows(ids, dout, stream=side)
+    side.synchronize()
+    assert np.array_equal(bits(a), bits(a2)) and np.array_equal(bits(b), bits(b2)) and np.array_equal(bits(r), bits(r2))
+    assert torch.equal(u, u2)
