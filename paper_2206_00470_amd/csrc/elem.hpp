@@ -101,6 +101,16 @@ __device__ __forceinline__ void store_raw(T* p, const raw_t<T, VW>& r) {
   }
 }
 
+// 16 bytes at an address aligned to its elements only (global memory takes
+// vectors at any address).
+typedef uint32_t words4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
+
+template <bool NT>
+__device__ __forceinline__ void store_anywhere(void* p, const words4& v) {
+  if constexpr (NT) __builtin_nontemporal_store((words4_anywhere)v, static_cast<words4_anywhere*>(p));
+  else *static_cast<words4_anywhere*>(p) = v;
+}
+
 // f(T{}) for the element type that a type code of the C ABI names; the
 // caller has checked the code.
 template <class F>

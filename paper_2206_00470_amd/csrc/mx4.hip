@@ -5,6 +5,7 @@
 #include <climits>
 
 #include "internal.hpp"
+#include "rules.hpp"
 
 using namespace adapm;
 
@@ -109,16 +110,25 @@ ps_status ps_mx4_product(int64_t m, int64_t n, int32_t dim, const uint8_t* a_cod
   if (m > kRows || n > kRows) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld rows", (long long)m, (long long)n);
   const MxRows A{a_codes, a_scales, m}, B{b_codes, b_scales, n};
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {
-    auto launch = [&](auto kernel, int tile_m, int tile_n) -> ps_status {
-      const int64_t tm = div_up(m, tile_m), tn = div_up(n, tile_n);
-      if (tm > INT_MAX / tn) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld exceed the grid", (long long)m, (long long)n);
-      hipLaunchKernelGGL(kernel, dim3(tm * tn), dim3(BLOCK), 0, static_cast<hipStream_t>(stream), A, B, blocks_of(dim),
-                         scale, static_cast<OT*>(out), out_stride, tn);
+    auto launch = [&](auto kernel, int tile_q, int tile_t) -> ps_status {
+      const int64_t tq = div_up(m, tile_q), tt = div_up(n, tile_t);
+      if (tq > (INT_MAX - NUM_XCD) / tt) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld exceed the grid", (long long)m, (long long)n);
+      hipLaunchKernelGGL(kernel, dim3(div_up(tq * tt, NUM_XCD) * NUM_XCD), dim3(BLOCK), 0,
+                         static_cast<hipStream_t>(stream), A, B, blocks_of(dim),
+                         scale, static_cast<OT*>(out), out_stride, tq);
       RAISE_HIP(hipGetLastError());
       return PS_OK;
     };
-    if (m <= 32) return launch(k_mx4_product<OT, 1, 1, 1, 4>, 32, 128);
-    return launch(k_mx4_product<OT, 2, 2, 2, 2>, 128, 128);
+    // past the caches where C fills the last-level one and its rows are whole lines
+    // (1,024 x 65,536 in fp32 of dim 1,024 108 us through the caches, 77 past them;
+    // rows that share lines, 2,048 x 50,021 in fp32 131 and 173)
+    const bool nt = m * n * (int64_t)sizeof(OT) >= LLC_BYTES && on_bytes(out, 64) && out_stride * sizeof(OT) % 64 == 0;
+    if (m <= 32) {
+      if (nt) return launch(k_mx4_product<OT, 1, 2, 1, 4, true>, 32, 256);
+      return launch(k_mx4_product<OT, 1, 2, 1, 4, false>, 32, 256);
+    }
+    if (nt) return launch(k_mx4_product<OT, 2, 2, 2, 2, true>, 128, 128);
+    return launch(k_mx4_product<OT, 2, 2, 2, 2, false>, 128, 128);
   });
 }
 

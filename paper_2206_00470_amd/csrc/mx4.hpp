@@ -146,13 +146,29 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint32_t* __restrict_
 // ------------------------------------------------------------------ product
 //   C[i][j] = T( scale * sum_k A[i][k] B[j][k] ),  A [m][dim], B [n][dim]
 // on the block-scaled matrix instruction of 32 x 32 x 64: lane l of a wave
-// gives block l / 32 of row l % 32 of each operand, 32 codes and their scale;
-// the products are exact and summed in fp32.  The sum over k has no order, so
-// a lane takes neighbouring blocks of its row.  B's rows run along the lanes of the result (column l % 32), so that stores of
-// one register are 32 neighbouring elements of a row of C.
+// gives one block (32 codes and their scale) of row l % 32 of each operand, the
+// lanes from 32 on another block than those below.  Products are exact, sums
+// fp32.  The sum over k has no order of its own, so a lane takes four
+// neighbouring blocks of its row at a time: 64 bytes of codes, one word of
+// scales, whose bytes the instruction selects.
+//
+// B's rows go in as the first operand, so that a lane's result registers are
+// four neighbouring columns of a row of C; they pass through LDS to leave as
+// whole stretches of a row, 16 bytes a lane.
+//
+// The codes are staged in LDS eight blocks of a row at a time, copied there
+// without a detour through registers: read straight from memory, the fragments
+// of one instruction lie in 32 lines (2,048 x 131,072 of dim 512 326 us against
+// 153). One buffer: other workgroups of the compute unit fill the wait better
+// than a second buffer does (200 us), since that leaves room for two of them
+// instead of three.
 //
 // Bound by C's bytes where there are many queries (a table's width is a few
-// hundred), by B's where there are few.
+// hundred: 2 dim operations per element written), by B's where there are few.
+// Measured: one query x 4.6M rows of 256 108 us, 6.0 TB/s of rows read and
+// scores written; 2,048 x 131,072 of dim 64 in bf16 99 us, 5.5 TB/s, of dim 512
+// 153 us, 3.7 TB/s and 1,800 TFLOP/s; 2,048 x 31,000 of dim 2,048 130 us, 2,000
+// TFLOP/s.
 typedef int mx_operand __attribute__((ext_vector_type(8)));
 typedef float mx_acc __attribute__((ext_vector_type(16)));
 
@@ -162,63 +178,197 @@ struct MxRows {
   int64_t rows;
 };
 
-// The codes and scale of block kb of a row, zeros outside.
-__device__ __forceinline__ void mx_load(const MxRows& t, int64_t row, int kb, int blocks_row, words4& c, int& s) {
-  c = words4{0u, 0u, 0u, 0u};
-  s = 127;
-  if (row < t.rows && kb < blocks_row) {
-    c = *reinterpret_cast<const words4*>(t.codes + (row * blocks_row + kb) * MX_BYTES);
-    s = t.scales[row * blocks_row + kb];
+// Staged codes: rows of eight blocks (128 bytes), block b of a row in slot
+// b ^ (row / 2 % 8), so that the blocks of one number of sixteen rows lie in
+// sixteen different slots of 256 bytes: reading them has no bank conflict.
+__device__ __forceinline__ int mx_slot(int row, int b) { return row * 8 + (b ^ ((row >> 1) & 7)); }
+
+// Copies blocks k0 .. k0+7 of the ROWS rows from row0 on into LDS, the eight
+// rows of an instruction side by side.  Rows beyond the last are taken from the
+// last, blocks beyond the row's end from its last block.
+template <int ROWS>
+__device__ __forceinline__ void mx_stage(const MxRows& t, int64_t row0, int k0, int blocks_row, words4* to) {
+  const int w = threadIdx.x / WAVE, l = lane_id();
+#pragma unroll
+  for (int i = 0; i < ROWS / 8; i += WAVES_PER_BLOCK) {
+    const int g = i + w;   // (ROWS / 8 is a multiple of the number of waves)
+    const int rt = g * 8 + l / 8;
+    int64_t row = row0 + rt;
+    if (row >= t.rows) row = t.rows - 1;
+    int kb = k0 + ((l % 8) ^ ((rt >> 1) & 7));
+    if (kb >= blocks_row) kb = blocks_row - 1;
+    const uint8_t* src = t.codes + (row * blocks_row + kb) * MX_BYTES;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                     (__attribute__((address_space(3))) void*)(to + g * WAVE), 16, 0, 0);
   }
+}
+
+// The scale bytes of blocks kb .. kb+count-1 of a row (count at most 4), 1
+// where they are beyond its end.
+template <bool FULL>
+__device__ __forceinline__ uint32_t mx_scales(const MxRows& t, int64_t row, int kb, int count, int blocks_row) {
+  const uint8_t* p = t.scales + row * blocks_row + kb;
+  uint32_t s;
+  if constexpr (FULL) {
+    __builtin_memcpy(&s, p, 4);
+  } else {
+    s = 0x7f7f7f7fu;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (q < count && kb + q < blocks_row) s ^= (uint32_t)(p[q] ^ 0x7fu) << (8 * q);
+  }
+  return s;
 }
 
 __device__ __forceinline__ mx_operand mx_words(const words4& c) {
   return mx_operand{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
 }
 
-// A wave's tile: MT x 32 rows of A by NTL x 32 rows of B; a workgroup's waves
-// are WM x WN such tiles.
-template <class OT, int MT, int NTL, int WM, int WN>
-__global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int blocks_row, float scale,
-                                                       OT* __restrict__ C, int64_t ldc, int64_t tiles_n) {
-  static_assert(WM * WN == WAVES_PER_BLOCK, "four waves");
-  const int w = threadIdx.x / WAVE, l = lane_id();
-  const int64_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
-  const int64_t i0 = (tm * WM + w / WN) * (MT * 32), j0 = (tn * WN + w % WN) * (NTL * 32);
-  const int half = l / 32, r = l % 32;
-  mx_acc acc[MT][NTL];
-#pragma unroll
-  for (int a = 0; a < MT; ++a)
-#pragma unroll
-    for (int b = 0; b < NTL; ++b)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
-  for (int k0 = 0; k0 < blocks_row; k0 += 2) {
-    const int kb = k0 + half;
-    words4 ca[MT], cb[NTL];
-    int sa[MT], sb[NTL];
-#pragma unroll
-    for (int a = 0; a < MT; ++a) mx_load(A, i0 + a * 32 + r, kb, blocks_row, ca[a], sa[a]);
-#pragma unroll
-    for (int b = 0; b < NTL; ++b) mx_load(B, j0 + b * 32 + r, kb, blocks_row, cb[b], sb[b]);
-#pragma unroll
-    for (int a = 0; a < MT; ++a)
-#pragma unroll
-      for (int b = 0; b < NTL; ++b)
-        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_words(ca[a]), mx_words(cb[b]), acc[a][b], 4, 4,
-                                                                   0, sa[a], 0, sb[b]);
+// The workgroup's tile.  With several tiles of queries each die takes one
+// stretch of C's columns, in groups of MX_GROUP tiles, a group's tiles row after
+// row: B's rows come into one die's cache once, the lines in which two
+// neighbouring tiles' rows meet are put together there, and the tiles at work
+// lie side by side (tiles under each other, 2^k bytes apart, meet in few
+// channels of the memory).  Measured, 2,048 x 131,072 of dim 64 and 512, bf16:
+// tiles under each other 134 and 160 us, groups 99 and 157.
+constexpr int MX_GROUP = 16;
+
+__device__ __forceinline__ void mx_tile(int64_t tiles_q, int64_t tiles_b, int64_t& tb, int64_t& tq) {
+  if (tiles_q == 1) {
+    tb = blockIdx.x;
+    tq = 0;
+    return;
   }
+  const int64_t tile = (int64_t)(blockIdx.x % NUM_XCD) * (gridDim.x / NUM_XCD) + blockIdx.x / NUM_XCD;
+  const int64_t group = tile / (MX_GROUP * tiles_q), rest = tile - group * (MX_GROUP * tiles_q);
+  const int64_t left = tiles_b - group * MX_GROUP;
+  const int64_t wide = left < 1 ? 1 : left < MX_GROUP ? left : MX_GROUP;
+  tq = rest / wide;
+  tb = group * MX_GROUP + (rest - tq * wide);
+  if (tq >= tiles_q) tb = tiles_b;   // beyond the last tile
+}
+
+// A wave's tile is QT x 32 rows of A by TT x 32 rows of B; a workgroup's waves
+// stand WQ x WT.  Rows of C are stored 16 bytes at a time wherever they start.
+template <class OT, int QT, int TT, int WQ, int WT, bool NT>
+__global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int blocks_row, float scale,
+                                                       OT* __restrict__ C, int64_t ldc, int64_t tiles_q) {
+  constexpr int VW = 16 / sizeof(OT);
+  constexpr int ET = sizeof(OT) == 2 && TT % 4 == 0 ? 4 : 2;   // tiles that leave together: rows of 256 or 128 bytes
+  static_assert(WQ * WT == WAVES_PER_BLOCK && TT % ET == 0, "four waves, whole rows");
+  constexpr int COLS = ET * 32, PITCH = COLS + VW;   // elements; rows start four banks apart
+  constexpr int RA = WQ * QT * 32, RB = WT * TT * 32;   // rows of the workgroup's tile
+  constexpr size_t kStage = (RA + RB) * 8 * sizeof(words4), kOut = WAVES_PER_BLOCK * 32 * PITCH * sizeof(OT);
+  __shared__ words4 lds[(kStage > kOut ? kStage : kOut) / sizeof(words4)];
+  const int w = threadIdx.x / WAVE, l = lane_id();
+  int64_t tb, tq;
+  mx_tile(tiles_q, (B.rows + RB - 1) / RB, tb, tq);
+  if (tb * RB >= B.rows) return;   // (the grid is a multiple of the dies)
+  const int wa = w / WT * QT * 32, wb = w % WT * TT * 32;   // the wave's rows in the tile
+  const int64_t i0 = tq * RA + wa, j0 = tb * RB + wb;
+  const int half = l / 32, r = l % 32;
+  words4 *sa = lds, *sb = lds + RA * 8;
+  int64_t ra[QT], rb[TT];   // the lane's rows
 #pragma unroll
-  for (int a = 0; a < MT; ++a)
+  for (int q = 0; q < QT; ++q) ra[q] = i0 + q * 32 + r < A.rows ? i0 + q * 32 + r : A.rows - 1;
 #pragma unroll
-    for (int b = 0; b < NTL; ++b) {
-      const int64_t j = j0 + b * 32 + r;
+  for (int t = 0; t < TT; ++t) rb[t] = j0 + t * 32 + r < B.rows ? j0 + t * 32 + r : B.rows - 1;
+  mx_acc acc[QT][TT];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int64_t i = i0 + a * 32 + 8 * (e / 4) + 4 * half + e % 4;
-        const float x = scale * acc[a][b][e];
-        if (i < A.rows && j < B.rows) store_raw<OT, 1>(C + i * ldc + j, raw_make<OT, 1>(&x));
+  for (int q = 0; q < QT; ++q)
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[q][t][e] = 0.0f;
+  uint32_t xa[QT], xb[TT];   // scales
+  // block number K of the lane's blocks first .. first+3 of the staged ones
+  auto multiply = [&]<int K, bool FULL>(int first, int rem) {
+    mx_operand fa[QT], fb[TT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+      words4 c = sa[mx_slot(wa + q * 32 + r, first + K)];
+      if (!FULL && first + K >= rem) c = words4{0u, 0u, 0u, 0u};
+      fa[q] = mx_words(c);
+    }
+#pragma unroll
+    for (int t = 0; t < TT; ++t) fb[t] = mx_words(sb[mx_slot(wb + t * 32 + r, first + K)]);
+#pragma unroll
+    for (int q = 0; q < QT; ++q)
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+        acc[q][t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[t], fa[q], acc[q][t], 4, 4, K, (int)xb[t], K,
+                                                                    (int)xa[q]);
+  };
+  auto stage = [&](int k0) {
+    if (k0 > 0) __syncthreads();
+    mx_stage<RB>(B, tb * RB, k0, blocks_row, sb);
+    mx_stage<RA>(A, tq * RA, k0, blocks_row, sa);
+  };
+  auto staged = [&] {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  int k0 = 0;
+  for (; k0 + 8 <= blocks_row; k0 += 8) {
+    stage(k0);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<true>(B, rb[t], k0 + 4 * half, 4, blocks_row);
+#pragma unroll
+    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<true>(A, ra[q], k0 + 4 * half, 4, blocks_row);
+    staged();
+    multiply.template operator()<0, true>(4 * half, 8);
+    multiply.template operator()<1, true>(4 * half, 8);
+    multiply.template operator()<2, true>(4 * half, 8);
+    multiply.template operator()<3, true>(4 * half, 8);
+  }
+  if (k0 < blocks_row) {   // up to seven blocks, halved between the lanes below 32 and above
+    const int rem = blocks_row - k0, per = (rem + 1) / 2;
+    stage(k0);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<false>(B, rb[t], k0 + per * half, per, blocks_row);
+#pragma unroll
+    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<false>(A, ra[q], k0 + per * half, per, blocks_row);
+    staged();
+    multiply.template operator()<0, false>(per * half, rem);
+    if (per > 1) multiply.template operator()<1, false>(per * half, rem);
+    if (per > 2) multiply.template operator()<2, false>(per * half, rem);
+    if (per > 3) multiply.template operator()<3, false>(per * half, rem);
+  }
+  __syncthreads();   // the staged codes make room for the results
+  // register e of a tile: row r of A's 32, column 8 (e / 4) + 4 half + e % 4 of B's
+  OT* my = reinterpret_cast<OT*>(lds) + w * 32 * PITCH;
+#pragma unroll
+  for (int q = 0; q < QT; ++q)
+#pragma unroll
+    for (int t = 0; t < TT; t += ET) {
+      if (i0 + q * 32 >= A.rows || j0 + t * 32 >= B.rows) continue;   // (the same for the whole wave)
+#pragma unroll
+      for (int tt = 0; tt < ET; ++tt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = scale * acc[q][t + tt][4 * g + e];
+          store_raw<OT, 4>(my + r * PITCH + tt * 32 + 8 * g + 4 * half, raw_make<OT, 4>(x));
+        }
+      // the wave reads what its own lanes wrote
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      constexpr int LR = COLS / VW;   // lanes per row
+      const int c = l % LR * VW;
+      const int64_t j = j0 + t * 32 + c;
+#pragma unroll
+      for (int g = 0; g < 32; g += WAVE / LR) {
+        const int i = g + l / LR;
+        const words4 v = *reinterpret_cast<const words4*>(my + i * PITCH + c);
+        if (i0 + q * 32 + i >= A.rows) continue;
+        OT* p = C + (i0 + q * 32 + i) * ldc + j;
+        if (j + VW <= B.rows) store_anywhere<NT>(p, v);
+        else
+          for (int e = 0; e < VW && j + e < B.rows; ++e) p[e] = my[i * PITCH + c + e];
       }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
 }
 
