@@ -16,9 +16,13 @@ __all__ = [*_STORE, *_OPERATORS, "workloads"]
 
 def __getattr__(name):
     if name in _STORE:
-        return getattr(importlib.import_module(__name__ + ".store"), name)
-    if name in _OPERATORS:
-        return getattr(importlib.import_module(__name__ + ".operators"), name)
-    if name == "workloads":
+        module = "store"
+    elif name in _OPERATORS:
+        module = "operators"
+    elif name == "workloads":
         return importlib.import_module(__name__ + ".workloads")
-    raise AttributeError(name)
+    else:
+        raise AttributeError(name)
+    value = getattr(importlib.import_module(__name__ + "." + module), name)
+    globals()[name] = value   # found without this function from now on
+    return value

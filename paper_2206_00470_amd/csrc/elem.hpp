@@ -25,17 +25,10 @@ typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 template <class T, int VW>
 using raw_t = typename Raw<T, VW>::type;
 
-template <class T, int VW, bool NT = false>
+// Loads and stores at addresses aligned to the vector.
+template <class T, int VW>
 __device__ __forceinline__ raw_t<T, VW> load_raw(const T* p) {
-  if constexpr (sizeof(T) * VW == 32) {   // two vectors: rows are aligned to 16 bytes
-    const words4* q = reinterpret_cast<const words4*>(p);
-    const words4 a = q[0], b = q[1];
-    return raw_t<T, VW>{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  } else if constexpr (NT) {
-    return __builtin_nontemporal_load(reinterpret_cast<const raw_t<T, VW>*>(p));
-  } else {
-    return *reinterpret_cast<const raw_t<T, VW>*>(p);
-  }
+  return *reinterpret_cast<const raw_t<T, VW>*>(p);
 }
 
 // Element e of the words.
@@ -84,31 +77,50 @@ __device__ __forceinline__ raw_t<T, VW> raw_make(const float* x) {
 
 template <class T, int VW, bool NT = false>
 __device__ __forceinline__ void store_raw(T* p, const raw_t<T, VW>& r) {
-  if constexpr (sizeof(T) * VW == 32) {
-    words4* q = reinterpret_cast<words4*>(p);
-    const words4 a = {r[0], r[1], r[2], r[3]}, b = {r[4], r[5], r[6], r[7]};
-    if constexpr (NT) {
-      __builtin_nontemporal_store(a, q);
-      __builtin_nontemporal_store(b, q + 1);
-    } else {
-      q[0] = a;
-      q[1] = b;
-    }
-  } else if constexpr (NT) {
-    __builtin_nontemporal_store(r, reinterpret_cast<raw_t<T, VW>*>(p));
+  if constexpr (NT) __builtin_nontemporal_store(r, reinterpret_cast<raw_t<T, VW>*>(p));
+  else *reinterpret_cast<raw_t<T, VW>*>(p) = r;
+}
+
+// The same in global memory at addresses that are aligned to their elements
+// only: global memory takes vectors of up to 16 bytes at any address.
+typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+template <class T, int VW>
+__device__ __forceinline__ raw_t<T, VW> load_any(const T* p) {
+  constexpr int bytes = sizeof(T) * VW;
+  if constexpr (bytes == 32) {
+    const words4_any *q = reinterpret_cast<const words4_any*>(p);
+    const words4 a = q[0], b = q[1];
+    return raw_t<T, VW>{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  } else if constexpr (bytes == 16) {
+    return *reinterpret_cast<const words4_any*>(p);
+  } else if constexpr (bytes == 8) {
+    return *reinterpret_cast<const words2_any*>(p);
   } else {
-    *reinterpret_cast<raw_t<T, VW>*>(p) = r;
+    return load_raw<T, VW>(p);
   }
 }
 
-// 16 bytes at an address aligned to its elements only (global memory takes
-// vectors at any address).
-typedef uint32_t words4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
+template <class V, bool NT>
+__device__ __forceinline__ void store_words(void* p, V v) {
+  if constexpr (NT) __builtin_nontemporal_store(v, static_cast<V*>(p));
+  else *static_cast<V*>(p) = v;
+}
 
-template <bool NT>
-__device__ __forceinline__ void store_anywhere(void* p, const words4& v) {
-  if constexpr (NT) __builtin_nontemporal_store((words4_anywhere)v, static_cast<words4_anywhere*>(p));
-  else *static_cast<words4_anywhere*>(p) = v;
+template <class T, int VW, bool NT = false>
+__device__ __forceinline__ void store_any(T* p, const raw_t<T, VW>& r) {
+  constexpr int bytes = sizeof(T) * VW;
+  if constexpr (bytes == 32) {
+    store_words<words4_any, NT>(p, words4{r[0], r[1], r[2], r[3]});
+    store_words<words4_any, NT>(reinterpret_cast<char*>(p) + 16, words4{r[4], r[5], r[6], r[7]});
+  } else if constexpr (bytes == 16) {
+    store_words<words4_any, NT>(p, r);
+  } else if constexpr (bytes == 8) {
+    store_words<words2_any, NT>(p, r);
+  } else {
+    store_raw<T, VW, NT>(p, r);
+  }
 }
 
 // f(T{}) for the element type that a type code of the C ABI names; the

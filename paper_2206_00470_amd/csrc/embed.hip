@@ -22,12 +22,6 @@ ps_status check_count(int64_t n) {
   return PS_OK;
 }
 
-// Whether rows of elements of `bytes` bytes at p, ld apart, can be accessed
-// vw elements (at most 16 bytes of them) at a time.
-bool rows_vector(const void* p, int64_t ld, int bytes, int vw) {
-  return ld % vw == 0 && on_bytes(p, std::min(vw * bytes, 16));
-}
-
 template <class F>
 ps_status with_width(int vw, F&& f) {
   if (vw == 8) return f.template operator()<8>();
@@ -49,24 +43,26 @@ ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, floa
   if (n == 0) return PS_OK;
   if (!ids || !out) return raise(PS_ERR_INVALID, "ids or out is NULL");
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int vb = t.bf16 ? 2 : 4, ob = type_bytes(out_type);
+  const int ob = type_bytes(out_type);
   if (!on_bytes(out, ob)) return raise(PS_ERR_INVALID, "out is not aligned to its elements");
-  auto fits = [&](int vw) {
-    return t.dim % vw == 0 && rows_vector(t.values, t.ld, vb, vw) && rows_vector(out, out_stride, ob, vw);
-  };
-  const int vw = fits(8) ? 8 : fits(4) ? 4 : 1;
-  const SmallDiv nv = small_div((uint32_t)(t.dim / vw));
+  // stores of 16 bytes (to bf16 from fp32 in vectors of four: 105 us instead of 89 as in lookup.hpp)
+  const int vw = t.dim >= 8 && ob == 2 ? 8 : t.dim >= 4 ? 4 : 1;
+  const SmallDiv nv = small_div((uint32_t)div_up(t.dim, vw));
   const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * EMBED_FLIGHT);
   if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the lookup's grid", (long long)n, t.dim);
   const LookupIds l{ids, n, pad, t.num_keys, t.map, t.map_keys, t.status};
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {
     return with_width(vw, [&]<int VW>() -> ps_status {
       auto launch = [&](auto kernel, auto values) {
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, st, values, t.ld, l, nv, scale, static_cast<OT*>(out),
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, st, values, t.ld, l, nv, t.dim, scale, static_cast<OT*>(out),
                            out_stride);
       };
-      if (t.bf16) launch(k_embed<bf16_t, OT, VW, false>, static_cast<const bf16_t*>(t.values));
-      else launch(k_embed<float, OT, VW, false>, static_cast<const float*>(t.values));
+      auto launch_values = [&]<class VT>(const VT* values) {
+        if (n * int64_t(t.dim) * ob > LOOKUP_STREAMS) launch(k_embed<VT, OT, VW, true>, values);
+        else launch(k_embed<VT, OT, VW, false>, values);
+      };
+      if (t.bf16) launch_values(static_cast<const bf16_t*>(t.values));
+      else launch_values(static_cast<const float*>(t.values));
       RAISE_HIP(hipGetLastError());
       return PS_OK;
     });
@@ -78,11 +74,21 @@ ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, floa
 // ======================================================================== gradient
 namespace {
 
+// Blocks folded together: a run over x blocks is finished from about x / f + f
+// partial rows, one after another; the commonest token has a tenth or so of a
+// batch.
+int fold_blocks(int64_t blocks) { return blocks < 16384 ? 16 : blocks < (1 << 20) ? 64 : 256; }
+
+// Positions of a block: fewer rows are added one after another where there are
+// not enough blocks of 16 to fill the units, which costs more partial rows.
+int block_of(int64_t n, int dim) { return n * int64_t(dim) < (int64_t(1) << 24) ? 8 : 16; }
+
 struct GradPlan {
   size_t order = 0;        // the sort's share, at the start
+  int block = 0;           // positions of a block
   double* partial = nullptr;
   double* fold = nullptr;
-  int32_t* split_list = nullptr;
+  int4* split_list = nullptr;
   uint32_t* split_count = nullptr;
   size_t bytes = 0;
 };
@@ -97,10 +103,11 @@ GradPlan plan_grad(void* ws, int64_t n, int dim) {
     off += bytes;
     return q;
   };
-  const int64_t blocks = div_up(n, GRAD_BLOCK);
+  p.block = block_of(n, dim);
+  const int64_t blocks = div_up(n, p.block);
   p.partial = reinterpret_cast<double*>(take(size_t(2) * blocks * dim * sizeof(double)));
-  p.fold = reinterpret_cast<double*>(take(size_t(blocks / GRAD_FOLD) * dim * sizeof(double)));
-  p.split_list = reinterpret_cast<int32_t*>(take(size_t(blocks) * sizeof(int32_t)));
+  p.fold = reinterpret_cast<double*>(take(size_t(blocks / fold_blocks(blocks)) * dim * sizeof(double)));
+  p.split_list = reinterpret_cast<int4*>(take(size_t(blocks) * sizeof(int4)));
   p.split_count = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
   p.bytes = off + 256;
   return p;
@@ -129,7 +136,7 @@ ps_status clear_rows(const GradOut& o, int64_t rows, int dim, hipStream_t st) {
   }
   const int vec = halves % 8 == 0 && ld % 8 == 0 && on_bytes(o.p, 16) ? 8
                   : halves % 2 == 0 && ld % 2 == 0 && on_bytes(o.p, 4) ? 2 : 1;
-  const int64_t grid = std::min<int64_t>(div_up(rows * (halves / vec), BLOCK * 4), 8192);
+  const int64_t grid = std::min<int64_t>(div_up(rows * (halves / vec), BLOCK), 8192);
   hipLaunchKernelGGL(k_grad_clear, dim3(grid), dim3(BLOCK), 0, st, static_cast<uint16_t*>(o.p), rows, halves, ld, vec);
   RAISE_HIP(hipGetLastError());
   return PS_OK;
@@ -163,15 +170,16 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
   if (ws_bytes < p.bytes) return raise(PS_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, p.bytes);
   if (!on_bytes(ws, 16)) return raise(PS_ERR_INVALID, "the workspace must be 16-byte aligned");
 
-  auto fits = [&](int vw) {
-    return t.dim % vw == 0 && rows_vector(c.dout, c.in_ld, ib, vw) && rows_vector(c.out.p, c.out.ld, ob, vw);
-  };
-  const int vw = ib == 2 && fits(8) ? 8 : fits(4) ? 4 : 1;
-  const int vectors = t.dim / vw;
+  // 16 bytes of the wider side; where sums are added to a row, vectors that lie
+  // over each other would add twice
+  const bool apart = c.out.accumulate != 0;
+  auto fits = [&](int w) { return apart ? t.dim % w == 0 : t.dim >= w; };
+  const int vw = ib + ob == 4 && fits(8) ? 8 : fits(4) ? 4 : 1;
+  const int vectors = (int)div_up(t.dim, vw);
   int lanes = 4;
   while (lanes < WAVE && lanes < vectors) lanes *= 2;
   const int slices = (int)div_up(vectors, lanes);
-  const int64_t blocks = div_up(c.n, GRAD_BLOCK);
+  const int64_t blocks = div_up(c.n, p.block);
   const int64_t grid = div_up(blocks * slices, BLOCK / lanes);
   if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld ids of %d exceed the merge's grid", (long long)c.n, t.dim);
 
@@ -181,11 +189,12 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
   if (ps_status r = order_ids(c.ids, c.n, c.pad, t.num_keys, ws, rows, c.uniq, p.split_count, t.status, st, &o))
     return r;
   const GradRuns g{o.keys, o.perm, c.n, (uint32_t)t.num_keys, rows ? o.seg_off : nullptr, o.hdr, c.num_unique,
-                   p.partial, p.split_list, p.split_count};
+                   p.partial, p.block, fold_blocks(blocks), p.split_list, p.split_count};
   const ps_status r = with_type(c.in_type, [&]<class IT>(IT) -> ps_status {
     return with_width(vw, [&]<int VW>() -> ps_status {
       if constexpr (sizeof(IT) * VW <= 16) {
-        hipLaunchKernelGGL((k_grad_merge<IT, VW>), dim3(grid), dim3(BLOCK), 0, st, g, static_cast<const IT*>(c.dout),
+        auto kernel = p.block == 8 ? k_grad_merge<IT, VW, 8> : k_grad_merge<IT, VW, 16>;
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), BLOCK / lanes * sizeof(GradMeta), st, g, static_cast<const IT*>(c.dout),
                            c.in_ld, t.dim, lanes, slices, (double)c.scale, c.out);
         RAISE_HIP(hipGetLastError());
       }
@@ -193,15 +202,15 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
     });
   });
   if (r) return r;
-  if (blocks < 2) return PS_OK;   // no run over several blocks
+  if (blocks < 3) return PS_OK;   // no run is longer than its block and the next
   const int col_slices = (int)div_up(t.dim, WAVE);
-  const int64_t supers = blocks / GRAD_FOLD;
+  const int64_t supers = blocks / fold_blocks(blocks);
   if (supers > 1) {   // (the first is never folded)
-    hipLaunchKernelGGL(k_grad_fold, dim3(std::min<int64_t>(supers * col_slices, 2048)), dim3(BLOCK), 0, st, g, supers,
+    hipLaunchKernelGGL(k_grad_fold, dim3(std::min<int64_t>(div_up(supers * col_slices, WAVES_PER_BLOCK), 2048)), dim3(BLOCK), 0, st, g, supers,
                        t.dim, col_slices, p.fold);
     RAISE_HIP(hipGetLastError());
   }
-  hipLaunchKernelGGL(k_grad_finish, dim3(std::min<int64_t>(blocks * col_slices, 2048)), dim3(BLOCK), 0, st, g, t.dim,
+  hipLaunchKernelGGL(k_grad_finish, dim3(std::min<int64_t>(div_up(blocks * col_slices, WAVES_PER_BLOCK), 2048)), dim3(BLOCK), 0, st, g, t.dim,
                      col_slices, p.fold, (double)c.scale, c.out);
   RAISE_HIP(hipGetLastError());
   return PS_OK;

@@ -12,10 +12,12 @@ namespace adapm {
 // written.  The rows are cut into vectors of VW elements and the vectors of
 // the whole output dealt out in order, EMBED_FLIGHT in flight per thread: every
 // lane has a vector whatever the row's width, a row of any width is spread
-// over as many workgroups as it fills, and a workgroup writes one stretch.
+// over as many workgroups as it fills, and a workgroup writes one stretch.  A
+// row that is no multiple of VW has its last vector end with the row, over some
+// elements of the one before: both write the same.
 template <class VT, class OT, int VW, bool NT>
 __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64_t ld, LookupIds l, SmallDiv nv,
-                                                 float scale, OT* __restrict__ out, int64_t out_ld) {
+                                                 int dim, float scale, OT* __restrict__ out, int64_t out_ld) {
   constexpr int U = EMBED_FLIGHT;
   const int64_t q0 = (int64_t)blockIdx.x * (BLOCK * U);
   const int64_t row0 = q0 / nv.d;
@@ -26,7 +28,8 @@ __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64
   for (int u = 0; u < U; ++u) {
     const uint32_t x = first + u * BLOCK;
     const uint32_t dr = quotient(x, nv);
-    const uint32_t c = (x - dr * nv.d) * VW;
+    const int at = (int)(x - dr * nv.d) * VW;
+    const int c = at + VW <= dim ? at : dim - VW;
     const int64_t i = row0 + dr;
     src[u] = -2;   // nothing to write
     if (i < l.n) {
@@ -39,7 +42,7 @@ __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     w[u] = raw_t<VT, VW>{};
-    if (src[u] >= 0) w[u] = load_raw<VT, VW>(W + src[u]);
+    if (src[u] >= 0) w[u] = load_any<VT, VW>(W + src[u]);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -47,7 +50,7 @@ __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64
     float x[VW];
 #pragma unroll
     for (int e = 0; e < VW; ++e) x[e] = src[u] < 0 ? 0.0f : scale * raw_get<VT, VW>(w[u], e);
-    store_raw<OT, VW, NT>(out + dst[u], raw_make<OT, VW>(x));
+    store_any<OT, VW, NT>(out + dst[u], raw_make<OT, VW>(x));
   }
   if (bad) atomicOr(l.err, 1);
   if (miss) atomicOr(l.err + 1, 1);
@@ -60,17 +63,16 @@ __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64
 // to the gradient's type (rounding twice costs at most 2^-24 of the value more
 // than rounding once).  No atomics: the sums have one order.
 //
-// The sorted positions are cut into blocks of GRAD_BLOCK, one row group of
+// The sorted positions are cut into blocks, one row group of
 // lanes per block and column slice, so that the rows in flight do not depend
 // on how long the runs are (most tokens of a batch come once or twice, the
-// commonest thousands of times).  A run inside a block is written at once.  A
-// run over several blocks leaves one fp64 partial row per block: in the even
-// slot of the block where it comes in from the block before or starts with the
+// commonest thousands of times).  A run inside a block is written at once, and
+// so is one that ends in the block after: the block where it starts takes it
+// whole.  A longer run leaves one fp64 partial row per block: in the even slot
+// of the block where it comes in from the block before or starts with the
 // block, in the odd slot where it starts inside.  k_grad_fold adds the even
-// slots of GRAD_FOLD blocks that one run fills, k_grad_finish adds the rest.
-constexpr int GRAD_BLOCK = 32;
-constexpr int GRAD_FOLD = 64;
-constexpr int GRAD_FLIGHT = 8;   // rows in flight per group
+// slots of `fold` blocks that one run fills, k_grad_finish adds the rest.
+constexpr int GRAD_BLOCK_MAX = 16;   // positions of a block: 16, or 8 in small calls
 
 // Where a token's gradient row goes: row `key` of the dense form, or the
 // run's index in the rows form (seg_off != NULL).
@@ -86,14 +88,14 @@ __device__ __forceinline__ void write_grad(const GradOut& o, int64_t row, int co
   OT* p = static_cast<OT*>(o.p) + row * o.ld + col;
   float x[VW];
   if (o.accumulate) {
-    const raw_t<OT, VW> old = load_raw<OT, VW>(p);
+    const raw_t<OT, VW> old = load_any<OT, VW>(p);
 #pragma unroll
     for (int e = 0; e < VW; ++e) x[e] = (float)((double)raw_get<OT, VW>(old, e) + scale * acc[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < VW; ++e) x[e] = (float)(scale * acc[e]);
   }
-  store_raw<OT, VW>(p, raw_make<OT, VW>(x));
+  store_any<OT, VW>(p, raw_make<OT, VW>(x));
 }
 
 template <int VW>
@@ -104,14 +106,21 @@ __device__ __forceinline__ void write_grad_any(const GradOut& o, int64_t row, in
   else write_grad<f16_t, VW>(o, row, col, acc, scale);
 }
 
-// Index of the run that holds sorted position p: the last u with
-// seg_off[u] <= p.
-__device__ __forceinline__ int32_t run_at(const int32_t* seg_off, int32_t num_runs, int32_t p) {
-  int32_t lo = 0, hi = num_runs;   // seg_off[lo] <= p < seg_off[hi]
-  while (hi - lo > 1) {
-    const int32_t mid = lo + (hi - lo) / 2;
-    if (seg_off[mid] <= p) lo = mid;
-    else hi = mid;
+// Index of the run that holds sorted position p, the last u with
+// seg_off[u] <= p, by the `lanes` lanes of a group together: each round they
+// probe as many places, so that a million runs take four rounds of 32 lanes
+// instead of twenty of one.
+__device__ __forceinline__ int32_t run_at(const int32_t* seg_off, int32_t num_runs, int32_t p, int lanes, int gl) {
+  int32_t lo = 0, len = num_runs;   // seg_off[lo] <= p < seg_off[lo + len]
+  const int shift = lane_id() - gl;
+  while (len > 1) {
+    const int32_t step = (len + lanes - 1) / lanes;
+    const int32_t at = (gl + 1) * step;
+    const bool below = at < len && seg_off[lo + at] <= p;
+    const uint64_t m = __ballot(below) >> shift;
+    const int k = __popcll(lanes == WAVE ? m : m & ((1ull << lanes) - 1));
+    lo += k * step;
+    len = len - k * step < step ? len - k * step : step;
   }
   return lo;
 }
@@ -125,62 +134,92 @@ struct GradRuns {
   const SegHeader* hdr;
   int32_t* num_unique;     // rows form: receives the number of rows
   double* partial;         // [2 * blocks][dim]
-  int32_t* split_list;     // first positions of the runs over several blocks
+  int block;               // positions of a block
+  int fold;                // blocks folded together
+  int4* split_list;        // the longer runs: first position, key, index of the run
   uint32_t* split_count;
 };
 
-template <class IT, int VW>
+// Keys and occurrences of a group's positions: its block, the one after and
+// the key behind them.
+struct GradMeta {
+  uint32_t key[2 * GRAD_BLOCK_MAX + 4];
+  uint32_t occ[2 * GRAD_BLOCK_MAX];
+};
+
+// All rows of a block are in flight at once and have arrived before the first
+// sum is written: the vector memory counter retires loads and stores in their
+// order, so a group that waited for a row behind a store would wait for the
+// store.  The positions of a run taken whole beyond the block are a second such
+// round.
+template <class IT, int VW, int BLK>
 __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __restrict__ dout, int64_t in_ld, int dim,
                                                       int lanes, int slices, double scale, GradOut out) {
-  constexpr int U = GRAD_FLIGHT;
+  constexpr int U = BLK;
+  extern __shared__ GradMeta grad_meta[];   // one per group
   const int64_t group = (int64_t)blockIdx.x * (BLOCK / lanes) + threadIdx.x / lanes;
   const int gl = threadIdx.x & (lanes - 1);
   const int64_t b = group / slices;
   const int slice = (int)(group - b * slices);
-  const int col = (slice * lanes + gl) * VW;
+  const int at = (slice * lanes + gl) * VW;
+  const bool active = at < dim;
+  const int col = at + VW <= dim ? at : dim - VW;   // the last vector ends with the row, as in k_embed
   if (g.seg_off && group == 0 && gl == 0) *g.num_unique = (int32_t)g.hdr->num_unique;
-  const int64_t p0 = b * GRAD_BLOCK;
+  const int64_t p0 = b * BLK;
   if (p0 >= g.n) return;
-  const int64_t p1 = p0 + GRAD_BLOCK < g.n ? p0 + GRAD_BLOCK : g.n;
-  uint32_t key = g.keys[p0];
-  if (key >= g.sentinel) return;
-  bool came_in = p0 > 0 && g.keys[p0 - 1] == key;   // the run began in an earlier block
-  int64_t start = p0;                               // the run's first position here
-  int64_t u = g.seg_off ? run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)p0) : 0;
-  const bool active = col < dim;
+  GradMeta& m = grad_meta[threadIdx.x / lanes];
+  for (int i = gl; i <= 2 * BLK; i += lanes) m.key[i] = p0 + i < g.n ? g.keys[p0 + i] : 0xffffffffu;
+  for (int i = gl; i < 2 * BLK; i += lanes) m.occ[i] = p0 + i < g.n ? g.perm[p0 + i] : 0u;
+  const uint32_t before = p0 > 0 ? g.keys[p0 - 1] : 0xffffffffu;
+  const uint32_t before2 = p0 > BLK ? g.keys[p0 - BLK - 1] : 0xffffffffu;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // a group's lanes are of one wave
+  __builtin_amdgcn_wave_barrier();
+  const int count = g.n - p0 < BLK ? (int)(g.n - p0) : BLK;
+  const uint32_t first = m.key[0], last = m.key[count - 1], next = m.key[count];
+  if (first >= g.sentinel) return;
+  bool came_in = before == first;                                     // the run began in an earlier block
+  const bool taken = came_in && before2 != first && next != first;    // which takes it whole
+  const bool extend = count == BLK && next == last && !(came_in && last == first) &&
+                      m.key[2 * BLK] != last;                  // as this block does its own last run
+  const int stop = extend ? 2 * BLK : count;
+  // (before the rows are asked for: behind them its loads would wait for them)
+  int32_t u = g.seg_off ? run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)p0, lanes, gl) : 0;
+  int start = 0;   // the run's first position here
+  const IT* src = dout + col;
   double acc[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) acc[e] = 0.0;
-  for (int64_t p = p0; p < p1; p += U) {
-    uint32_t k[U + 1], r[U];
-#pragma unroll
-    for (int i = 0; i <= U; ++i) k[i] = p + i < g.n ? g.keys[p + i] : 0xffffffffu;
-#pragma unroll
-    for (int i = 0; i < U; ++i) r[i] = p + i < g.n ? g.perm[p + i] : 0u;
+  for (int p = 0; p < stop; p += U) {
     raw_t<IT, VW> x[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       x[i] = raw_t<IT, VW>{};
-      if (active && k[i] < g.sentinel) x[i] = load_raw<IT, VW>(dout + (int64_t)r[i] * in_ld + col);
+      const uint32_t k = m.key[p + i];
+      if (active && k < g.sentinel && !(taken && k == first) && (p == 0 || k == last))
+        x[i] = load_any<IT, VW>(src + (int64_t)m.occ[p + i] * in_ld);
     }
 #pragma unroll
+    for (int i = 0; i < U; ++i) asm volatile("" : "+v"(x[i]));
+#pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (k[i] >= g.sentinel) return;   // the rest are too, and the last run has been written
+      const uint32_t k = m.key[p + i];
+      if (k >= g.sentinel || (p > 0 && k != last)) return;   // nothing of this group's follows
 #pragma unroll
       for (int e = 0; e < VW; ++e) acc[e] += (double)raw_get<IT, VW>(x[i], e);
-      const bool ends = k[i + 1] != k[i];
-      const bool leaves = !ends && p + i + 1 == p1;
+      const bool ends = m.key[p + i + 1] != k;
+      const bool leaves = !ends && p + i + 1 == count && !extend;
       if (!ends && !leaves) continue;
-      if (ends && !came_in) {
-        if (active) write_grad_any<VW>(out, g.seg_off ? u : (int64_t)k[i], col, acc, scale);
+      if (taken && k == first) {
+      } else if (ends && !came_in) {
+        if (active) write_grad_any<VW>(out, g.seg_off ? (int64_t)u : (int64_t)k, col, acc, scale);
       } else {
         if (active) {
-          double* q = g.partial + (2 * b + (start != p0 ? 1 : 0)) * dim + col;
+          double* q = g.partial + (2 * b + (start != 0 ? 1 : 0)) * dim + col;
 #pragma unroll
           for (int e = 0; e < VW; ++e) q[e] = acc[e];
         }
         if (leaves && !came_in && gl == 0 && slice == 0)
-          g.split_list[atomicAdd(g.split_count, 1u)] = (int32_t)start;
+          g.split_list[atomicAdd(g.split_count, 1u)] = int4{(int)p0 + start, (int)k, u, 0};
       }
 #pragma unroll
       for (int e = 0; e < VW; ++e) acc[e] = 0.0;
@@ -191,91 +230,97 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
   }
 }
 
-// Adds rows row(k), k = 0 .. count-1, of fp64 columns col, by the block's
-// four waves (wave w the rows w, w + 4, ..., FU in flight, then the waves'
-// sums in wave order); the total is valid in wave 0.
+// Adds rows row(k), k = 0 .. count-1, of fp64 column col in their order, FU of
+// them in flight.
 template <class RowAt>
-__device__ __forceinline__ double sum_rows_by_waves(RowAt row, int64_t count, bool active, int col, double* smem) {
-  constexpr int FU = 8;
-  const int w = threadIdx.x / WAVE;
+__device__ __forceinline__ double sum_rows(RowAt row, int64_t count, bool active, int col) {
+  constexpr int FU = 16;
   double acc = 0.0;
-  int64_t k = w;
-  for (; k + (FU - 1) * WAVES_PER_BLOCK < count; k += FU * WAVES_PER_BLOCK) {
+  int64_t k = 0;
+  for (; k + FU <= count; k += FU) {
     double x[FU];
 #pragma unroll
-    for (int f = 0; f < FU; ++f) x[f] = active ? row(k + f * WAVES_PER_BLOCK)[col] : 0.0;
+    for (int f = 0; f < FU; ++f) x[f] = active ? row(k + f)[col] : 0.0;
 #pragma unroll
     for (int f = 0; f < FU; ++f) acc += x[f];
   }
-  for (; k < count; k += WAVES_PER_BLOCK) acc += active ? row(k)[col] : 0.0;
-  smem[threadIdx.x] = acc;
-  __syncthreads();
-  double t = 0.0;
-  if (w == 0)
+  if (k < count) {
+    double x[FU];
 #pragma unroll
-    for (int i = 0; i < WAVES_PER_BLOCK; ++i) t += smem[i * WAVE + lane_id()];
-  __syncthreads();
-  return t;
+    for (int f = 0; f < FU; ++f) x[f] = active && k + f < count ? row(k + f)[col] : 0.0;
+#pragma unroll
+    for (int f = 0; f < FU; ++f)
+      if (k + f < count) acc += x[f];
+  }
+  return acc;
 }
 
-// fold[s] = the even slots of blocks [s * GRAD_FOLD, (s + 1) * GRAD_FOLD)
+// fold[s] = the even slots of blocks [s * g.fold, (s + 1) * g.fold)
 // where one run comes into the first of them and into the last (so into all).
+// One wave per column slice, here and below.
 __global__ __launch_bounds__(BLOCK) void k_grad_fold(GradRuns g, int64_t supers, int dim, int slices,
                                                      double* __restrict__ fold) {
-  __shared__ double smem[BLOCK];
-  for (int64_t e = blockIdx.x; e < supers * slices; e += gridDim.x) {
+  const int64_t step = (int64_t)gridDim.x * WAVES_PER_BLOCK;
+  for (int64_t e = (int64_t)blockIdx.x * WAVES_PER_BLOCK + threadIdx.x / WAVE; e < supers * slices; e += step) {
     const int64_t s = e / slices;
     const int col = (int)(e - s * slices) * WAVE + lane_id();
-    const int64_t b0 = s * GRAD_FOLD;
+    const int64_t b0 = s * g.fold;
     if (b0 == 0) continue;
-    const uint32_t key = g.keys[b0 * GRAD_BLOCK];   // uniform over the block, as what follows
-    if (key >= g.sentinel || g.keys[b0 * GRAD_BLOCK - 1] != key ||
-        g.keys[(b0 + GRAD_FOLD - 1) * GRAD_BLOCK] != key)
+    const uint32_t key = g.keys[b0 * g.block];
+    if (key >= g.sentinel || g.keys[b0 * g.block - 1] != key ||
+        g.keys[(b0 + g.fold - 1) * g.block] != key)
       continue;
-    const double t = sum_rows_by_waves([&](int64_t k) { return g.partial + 2 * (b0 + k) * dim; }, GRAD_FOLD,
-                                       col < dim, col, smem);
-    if (threadIdx.x < WAVE && col < dim) fold[s * dim + col] = t;
+    const double t = sum_rows([&](int64_t k) { return g.partial + 2 * (b0 + k) * dim; }, g.fold, col < dim, col);
+    if (col < dim) fold[s * dim + col] = t;
   }
+}
+
+// The last block that the run of `key`, which comes into block f, comes into;
+// most runs are short, so the steps double from there on.
+__device__ __forceinline__ int64_t last_block(const GradRuns& g, uint32_t key, int64_t f) {
+  const int64_t blocks = (g.n + g.block - 1) / g.block;
+  int64_t lo = f, hi = blocks;   // it comes into lo, not into hi
+  for (int64_t step = 1; lo + step < blocks; step *= 2) {
+    if (g.keys[(lo + step) * g.block] != key) {
+      hi = lo + step;
+      break;
+    }
+    lo += step;
+  }
+  while (hi - lo > 1) {
+    const int64_t mid = lo + (hi - lo) / 2;
+    if (g.keys[mid * g.block] == key) lo = mid;
+    else hi = mid;
+  }
+  return lo;
 }
 
 // The runs over several blocks: partial of the first block, of the blocks up
 // to the first folded ones, the folds, and the blocks after them, added in
-// this order by sum_rows_by_waves.
+// this order.
 __global__ __launch_bounds__(BLOCK) void k_grad_finish(GradRuns g, int dim, int slices,
                                                        const double* __restrict__ fold, double scale, GradOut out) {
-  __shared__ double smem[BLOCK];
   const int64_t items = (int64_t)*g.split_count * slices;
-  for (int64_t e = blockIdx.x; e < items; e += gridDim.x) {
+  const int64_t step = (int64_t)gridDim.x * WAVES_PER_BLOCK;
+  for (int64_t e = (int64_t)blockIdx.x * WAVES_PER_BLOCK + threadIdx.x / WAVE; e < items; e += step) {
     const int64_t r = e / slices;
     const int col = (int)(e - r * slices) * WAVE + lane_id();
-    const int64_t s0 = g.split_list[r];
-    const uint32_t key = g.keys[s0];
-    int64_t u = key, s1;
-    if (g.seg_off) {
-      u = run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)s0);
-      s1 = g.seg_off[u + 1];
-    } else {   // the first position with a larger key
-      int64_t lo = s0, hi = g.n;
-      while (hi - lo > 1) {
-        const int64_t mid = lo + (hi - lo) / 2;
-        if (g.keys[mid] <= key) lo = mid;
-        else hi = mid;
-      }
-      s1 = hi;
-    }
-    const int64_t f = s0 / GRAD_BLOCK + 1, l = (s1 - 1) / GRAD_BLOCK;   // blocks it comes into
-    const int64_t sa = (f + GRAD_FOLD - 1) / GRAD_FOLD, sb = (l + 1) / GRAD_FOLD;
+    const int4 run = g.split_list[r];
+    const int64_t s0 = run.x;
+    const uint32_t key = (uint32_t)run.y;
+    const int64_t f = s0 / g.block + 1, l = last_block(g, key, f);   // the blocks it comes into
+    const int64_t sa = (f + g.fold - 1) / g.fold, sb = (l + 1) / g.fold;
     const int64_t nf = sb > sa ? sb - sa : 0;
-    const int64_t n1 = nf ? sa * GRAD_FOLD - f : l - f + 1;
-    const int64_t n3 = nf ? l - sb * GRAD_FOLD + 1 : 0;
+    const int64_t n1 = nf ? sa * g.fold - f : l - f + 1;
+    const int64_t n3 = nf ? l - sb * g.fold + 1 : 0;
     auto row = [&](int64_t k) -> const double* {
-      if (k == 0) return g.partial + (2 * (s0 / GRAD_BLOCK) + (s0 % GRAD_BLOCK != 0 ? 1 : 0)) * dim;
+      if (k == 0) return g.partial + (2 * (s0 / g.block) + (s0 % g.block != 0 ? 1 : 0)) * dim;
       if (k <= n1) return g.partial + 2 * (f + k - 1) * dim;
       if (k <= n1 + nf) return fold + (sa + k - 1 - n1) * dim;
-      return g.partial + 2 * (sb * GRAD_FOLD + k - 1 - n1 - nf) * dim;
+      return g.partial + 2 * (sb * g.fold + k - 1 - n1 - nf) * dim;
     };
-    const double t = sum_rows_by_waves(row, 1 + n1 + nf + n3, col < dim, col, smem);
-    if (threadIdx.x < WAVE && col < dim) write_grad_any<1>(out, u, col, &t, scale);
+    const double t = sum_rows(row, 1 + n1 + nf + n3, col < dim, col);
+    if (col < dim) write_grad_any<1>(out, g.seg_off ? (int64_t)run.z : (int64_t)key, col, &t, scale);
   }
 }
 

@@ -54,11 +54,6 @@ ADAPM_HIDDEN size_t order_bytes(int64_t n);
 ADAPM_HIDDEN ps_status order_ids(const int64_t* ids, int64_t n, int64_t pad, int64_t num_keys, void* ws, bool runs,
                                  int64_t* uniq, uint32_t* counter, int32_t* err, hipStream_t st, Order* out);
 
-// Work enqueued on *side after fork_side runs beside what is then enqueued on
-// st; join_side makes st wait for it.  The stream is the store's second one.
-ADAPM_HIDDEN ps_status fork_side(ps_store* s, hipStream_t st, hipStream_t* side);
-ADAPM_HIDDEN ps_status join_side(ps_store* s, hipStream_t st);
-
 // Largest number of occurrences of one call.
 constexpr int64_t OCC_MAX = (int64_t(1) << 31) - (int64_t(1) << 20);
 

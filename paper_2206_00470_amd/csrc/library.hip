@@ -51,19 +51,38 @@ ps_status order_ids(const int64_t* ids, int64_t n, int64_t pad, int64_t num_keys
   Carver c(ws);
   carve_sort(c, n, 1, false, true, &b);
   uint32_t *ks, *perm;
-  (void)runs;
+  if (!runs && n > SMALL_KEYS_MAX) {
+    // the sort alone: run_keywork's without its last kernels
+    const KeysPadded keys{ids, pad, counter};
+    if (n > MID_KEYS_MAX) {
+      if (ps_status r = run_sort(nullptr, keys, n, num_keys, b, err, nullptr, false, st, &ks, &perm)) return r;
+      *out = Order{ks, perm, nullptr, nullptr};
+      return PS_OK;
+    }
+    const RadixPlan plan = radix_plan(num_keys);
+    const int tiles = (int)ceil_div(n, MID_TILE);
+    hipLaunchKernelGGL((k_mid_intake<KeysPadded>), dim3(tiles), dim3(SMALL_BLOCK), 0, st, keys, (int)n,
+                       (uint32_t)num_keys, plan.bits[0], b.k[0], b.counts, err);
+    LAUNCHED(k_mid_intake);
+    for (int p = 0; p < plan.passes; ++p) {
+      if (p > 0) {
+        hipLaunchKernelGGL(k_mid_count, dim3(tiles), dim3(SMALL_BLOCK), 0, st, b.k[p % 2], (int)n, plan.shift[p],
+                           plan.bits[p], b.counts);
+        LAUNCHED(k_mid_count);
+      }
+      hipLaunchKernelGGL(k_mid_scatter, dim3(tiles), dim3(SMALL_BLOCK), 0, st, b.k[p % 2],
+                         p > 0 ? b.v[p % 2] : nullptr, (int)n, plan.shift[p], plan.bits[p], b.counts, tiles,
+                         b.k[1 - p % 2], b.v[1 - p % 2], nullptr);
+      LAUNCHED(k_mid_scatter);
+    }
+    *out = Order{b.k[plan.passes % 2], b.v[plan.passes % 2], nullptr, nullptr};
+    return PS_OK;
+  }
   if (ps_status r = run_keywork(nullptr, KeysPadded{ids, pad, counter}, n, num_keys, b, err, nullptr, false, st, &ks,
                                 &perm, false, b.seg_off, uniq))
     return r;
   *out = Order{ks, perm, b.seg_off, b.hdr};
   return PS_OK;
 }
-
-ps_status fork_side(ps_store* s, hipStream_t st, hipStream_t* side) {
-  *side = s->aux;
-  return fork_aux(s, st);
-}
-
-ps_status join_side(ps_store* s, hipStream_t st) { return join_aux(s, st); }
 
 }  // namespace adapm

@@ -5,7 +5,19 @@
 
 namespace adapm {
 
-constexpr int EMBED_FLIGHT = 4;   // vectors in flight per thread
+// Vectors in flight per thread, of an fp32 or bf16 table and of a 4-bit one,
+// whose address takes longer to work out: 65,536 rows of 2,048 floats to bf16
+// 106 us with four, 89 with two or one; a table of 4.6M x 256 4-bit values
+// restored to bf16 587 with one, 516 with two, 491 with four.
+constexpr int EMBED_FLIGHT = 2;
+constexpr int MX4_FLIGHT = 4;
+
+// Outputs beyond this are written past the caches. Measured, through them and
+// past them, a lookup alone and with a kernel behind it that reads the output:
+// 61 MB (rows of 512 floats to bf16) 24.7 and 21.6 us, 47.2 and 48.9; 85 MB (100
+// floats) 33.0 and 23.5, 60.5 and 61.0; 127 MB (300 4-bit values to bf16) 50.6
+// and 33.1, 95.4 and 87.4; 240 MB (301 floats) 96.8 and 57.5, 178 and 164.
+constexpr int64_t LOOKUP_STREAMS = int64_t(80) << 20;
 
 struct LookupIds {
   const int64_t* ids;   // NULL: row i of the table

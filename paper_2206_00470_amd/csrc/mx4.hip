@@ -5,6 +5,7 @@
 #include <climits>
 
 #include "internal.hpp"
+#include "lookup.hpp"
 #include "rules.hpp"
 
 using namespace adapm;
@@ -44,15 +45,10 @@ ps_status ps_mx4_quantize(int64_t rows, int32_t dim, int32_t type, const void* x
   if (rows > INT64_MAX / (4 * per_row.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)rows);
   const int64_t grid = div_up(rows * per_row.d, int64_t(BLOCK) * QUANT_FLIGHT);
   if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)rows, dim);
-  const bool vec = dim % 8 == 0 && row_stride % 8 == 0 && on_bytes(x, 16);
   return with_type(type, [&]<class T>(T) -> ps_status {
-    auto launch = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
-                         static_cast<const T*>(x), rows, dim, row_stride, per_row, reinterpret_cast<uint32_t*>(codes),
-                         scales);
-    };
-    if (vec) launch(k_mx4_quantize<T, true>);
-    else launch(k_mx4_quantize<T, false>);
+    hipLaunchKernelGGL(k_mx4_quantize<T>, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
+                       static_cast<const T*>(x), rows, dim, row_stride, per_row, reinterpret_cast<uint32_t*>(codes),
+                       scales);
     RAISE_HIP(hipGetLastError());
     return PS_OK;
   });
@@ -73,22 +69,19 @@ ps_status ps_mx4_embed(const uint8_t* codes, const uint8_t* scales, int64_t num_
   if (!on_bytes(codes, 16)) return raise(PS_ERR_INVALID, "codes must be 16-byte aligned");
   const int b = type_bytes(out_type);
   if (!on_bytes(out, b)) return raise(PS_ERR_INVALID, "out is not aligned to its elements");
-  auto fits = [&](int vw) { return dim % vw == 0 && out_stride % vw == 0 && on_bytes(out, std::min(vw * b, 16)); };
-  const int vw = fits(8) ? 8 : fits(4) ? 4 : 1;
-  const SmallDiv nv = small_div((uint32_t)((dim + 7) / 8));
+  const SmallDiv nv = small_div((uint32_t)div_up(dim, 16 / b));
   if (n > INT64_MAX / (4 * nv.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)n);
-  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * EMBED_FLIGHT);
+  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * MX4_FLIGHT);
   if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)n, dim);
   const LookupIds l{ids, n, pad, num_rows, nullptr, 0, err};
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {
     auto launch = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
-                         reinterpret_cast<const uint32_t*>(codes), scales, blocks_of(dim), dim, l, nv, scale,
+                         codes, scales, blocks_of(dim), dim, l, nv, scale,
                          static_cast<OT*>(out), out_stride);
     };
-    if (vw == 8) launch(k_mx4_embed<OT, 8>);
-    else if (vw == 4) launch(k_mx4_embed<OT, 4>);
-    else launch(k_mx4_embed<OT, 1>);
+    if (n * int64_t(dim) * b > LOOKUP_STREAMS) launch(k_mx4_embed<OT, true>);
+    else launch(k_mx4_embed<OT, false>);
     RAISE_HIP(hipGetLastError());
     return PS_OK;
   });

@@ -30,7 +30,7 @@ __device__ __forceinline__ float scale_value(uint32_t s) {
 // float without its sign order like its value, infinities and NaN last).
 constexpr int QUANT_FLIGHT = 2;
 
-template <class T, bool VEC>
+template <class T>
 __global__ __launch_bounds__(BLOCK) void k_mx4_quantize(const T* __restrict__ x, int64_t rows, int dim, int64_t ld,
                                                         SmallDiv per_row, uint32_t* __restrict__ codes,
                                                         uint8_t* __restrict__ scales) {
@@ -48,14 +48,14 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_quantize(const T* __restrict__ x,
     row[u] = row0 + dr;
     const T* p = x + row[u] * ld + c;
     const bool in = row[u] < rows;
-    if constexpr (VEC) {   // rows are whole vectors of eight
-      raw_t<T, 8> w{};
-      if (in && c < dim) w = load_raw<T, 8>(p);
+    raw_t<T, 8> w{};
+    if (in && c + 8 <= dim) w = load_any<T, 8>(p);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] = raw_get<T, 8>(w, e);
-    } else {
+    for (int e = 0; e < 8; ++e) v[u][e] = raw_get<T, 8>(w, e);
+    if (in && c < dim && c + 8 > dim) {   // the row's last few
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] = in && c + e < dim ? raw_get<T, 1>(load_raw<T, 1>(p + e), 0) : 0.0f;
+      for (int e = 0; e < 7; ++e)
+        if (c + e < dim) v[u][e] = raw_get<T, 1>(load_raw<T, 1>(p + e), 0);
     }
   }
 #pragma unroll
@@ -89,18 +89,19 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_quantize(const T* __restrict__ x,
 }
 
 // ------------------------------------------------------------------ lookup
-// As k_embed over quantised rows, eight codes (one word) of a row per vector
-// and stores of VW elements; ids NULL restores the whole table.
-template <class OT, int VW>
-__global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint32_t* __restrict__ codes,
+// As k_embed over quantised rows, vectors of 16 bytes of the output (eight
+// codes, or four); ids NULL restores the whole table.
+template <class OT, bool NT>
+__global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__ codes,
                                                      const uint8_t* __restrict__ scales, int blocks_row, int dim,
                                                      LookupIds l, SmallDiv nv, float scale, OT* __restrict__ out,
                                                      int64_t out_ld) {
-  constexpr int U = EMBED_FLIGHT;
+  constexpr int U = MX4_FLIGHT;
   const int64_t q0 = (int64_t)blockIdx.x * (BLOCK * U);
   const int64_t row0 = q0 / nv.d;
   const uint32_t first = (uint32_t)(q0 - row0 * nv.d) + threadIdx.x;
   int bad = 0, miss = 0;
+  constexpr int VW = 16 / sizeof(OT);
   uint32_t w[U], s[U];
   int64_t at[U];
   int col[U];
@@ -108,18 +109,20 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint32_t* __restrict_
   for (int u = 0; u < U; ++u) {
     const uint32_t x = first + u * BLOCK;
     const uint32_t dr = quotient(x, nv);
-    const uint32_t c = x - dr * nv.d;   // word of the row
+    const uint32_t c = (x - dr * nv.d) * VW;
     const int64_t i = row0 + dr;
     col[u] = dim;   // nothing to write
     w[u] = 0;
     s[u] = 0;
     if (i < l.n) {
-      col[u] = (int)c * 8;
-      at[u] = i * out_ld + col[u];
+      col[u] = (int)c;
+      at[u] = i * out_ld + c;
       const int64_t r = lookup_row(l, i, bad, miss);
       if (r >= 0) {
-        w[u] = codes[r * blocks_row * 4 + c];
-        s[u] = scales[r * blocks_row + (c >> 2)];
+        const uint8_t* p = codes + (r * blocks_row * MX_BYTES + c / 2);
+        if constexpr (VW == 8) w[u] = *reinterpret_cast<const uint32_t*>(p);
+        else w[u] = *reinterpret_cast<const uint16_t*>(p);
+        s[u] = scales[r * blocks_row + c / MX_BLOCK];
       }
     }
   }
@@ -127,17 +130,20 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint32_t* __restrict_
   for (int u = 0; u < U; ++u) {
     if (col[u] >= dim) continue;
     const float f = scale_value(s[u]);
-    float x[8];
+    float x[VW];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < VW; ++e) {
       // the magnitude's bits below an exponent of zero are its value / 2^126
       const uint32_t m = (w[u] >> (4 * e)) & 7u, sign = (w[u] >> (4 * e + 3)) << 31;
       x[e] = __builtin_bit_cast(float, m << 22 | sign) * 0x1p126f * f * scale;
     }
     const int left = dim - col[u];
+    if (left >= VW) {
+      store_any<OT, VW, NT>(out + at[u], raw_make<OT, VW>(x));
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; e += VW) {
-      if (e < left) store_raw<OT, VW>(out + at[u] + e, raw_make<OT, VW>(x + e));
+      for (int e = 0; e < VW - 1; ++e)
+        if (e < left) store_raw<OT, 1>(out + at[u] + e, raw_make<OT, 1>(x + e));
     }
   }
   if (bad) atomicOr(l.err, 1);
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int b
         const words4 v = *reinterpret_cast<const words4*>(my + i * PITCH + c);
         if (i0 + q * 32 + i >= A.rows) continue;
         OT* p = C + (i0 + q * 32 + i) * ldc + j;
-        if (j + VW <= B.rows) store_anywhere<NT>(p, v);
+        if (j + VW <= B.rows) store_words<words4_any, NT>(p, v);
         else
           for (int e = 0; e < VW && j + e < B.rows; ++e) p[e] = my[i * PITCH + c + e];
       }

@@ -68,15 +68,20 @@ class _On:
     (the device's current one if none is given) the one that new tensors
     belong to."""
 
+    __slots__ = ("device", "inner")
+
     def __init__(self, device, stream):
-        self.device, self.stream, self.inner = device, stream, None
-        if stream is not None or torch.cuda.current_device() != device.index:
-            self.inner = torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device))
+        self.device, self.inner = device, None
+        if stream is not None:
+            self.inner = torch.cuda.stream(stream)
+        elif torch.cuda.current_device() != device.index:
+            self.inner = torch.cuda.device(device)
 
     def __enter__(self):
         if self.inner is not None:
             self.inner.__enter__()
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+        # (the handle alone: a tenth of the time of torch.cuda.current_stream)
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def __exit__(self, *a):
         if self.inner is not None:
