@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "internal.hpp"
+#include "rules.hpp"
 
 using namespace adapm;
 
@@ -105,8 +106,12 @@ ps_status clip(int32_t count, const void* const* grads, void* const* outs, const
     RAISE_HIP(hipGetLastError());
     return PS_OK;
   }
-  for (size_t i = 0; i < lists.size(); ++i) {
-    hipLaunchKernelGGL(k_clip_scale, dim3(grid(lists[i])), dim3(BLOCK), 0, st, lists[i], part, parts, max_norm,
+  int64_t bytes = 0;   // written apart from what is read
+  for (int32_t i = 0; i < count; ++i)
+    if (grads[i] != outs[i]) bytes += numel[i] * type_bytes(types[i]);
+  auto kernel = bytes > LLC_BYTES / 2 ? k_clip_scale<true> : k_clip_scale<false>;
+  for (size_t i = lists.size(); i-- > 0;) {
+    hipLaunchKernelGGL(kernel, dim3(grid(lists[i])), dim3(BLOCK), 0, st, lists[i], part, parts, max_norm,
                        i == 0 ? norm : nullptr);
     RAISE_HIP(hipGetLastError());
   }

@@ -43,10 +43,11 @@ ps_status ps_mx4_quantize(int64_t rows, int32_t dim, int32_t type, const void* x
   if (!on_bytes(codes, 16)) return raise(PS_ERR_INVALID, "codes must be 16-byte aligned");
   const SmallDiv per_row = small_div((uint32_t)blocks_of(dim) * 4);
   if (rows > INT64_MAX / (4 * per_row.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)rows);
-  const int64_t grid = div_up(rows * per_row.d, int64_t(BLOCK) * QUANT_FLIGHT);
+  const int64_t grid = div_up(rows * per_row.d, BLOCK);
   if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)rows, dim);
   return with_type(type, [&]<class T>(T) -> ps_status {
-    hipLaunchKernelGGL(k_mx4_quantize<T>, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
+    auto kernel = rows * per_row.d * 4 > LOOKUP_STREAMS ? k_mx4_quantize<T, true> : k_mx4_quantize<T, false>;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
                        static_cast<const T*>(x), rows, dim, row_stride, per_row, reinterpret_cast<uint32_t*>(codes),
                        scales);
     RAISE_HIP(hipGetLastError());
