@@ -90,6 +90,8 @@ struct GradPlan {
   double* fold = nullptr;
   int4* split_list = nullptr;
   uint32_t* split_count = nullptr;
+  uint32_t* tile_heads = nullptr;   // rows form
+  int32_t* block_run = nullptr;
   size_t bytes = 0;
 };
 
@@ -109,6 +111,8 @@ GradPlan plan_grad(void* ws, int64_t n, int dim) {
   p.fold = reinterpret_cast<double*>(take(size_t(blocks / fold_blocks(blocks)) * dim * sizeof(double)));
   p.split_list = reinterpret_cast<int4*>(take(size_t(blocks) * sizeof(int4)));
   p.split_count = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
+  p.tile_heads = reinterpret_cast<uint32_t*>(take(size_t(div_up(n, RUNS_TILE)) * sizeof(uint32_t)));
+  p.block_run = reinterpret_cast<int32_t*>(take(size_t(blocks) * sizeof(int32_t)));
   p.bytes = off + 256;
   return p;
 }
@@ -185,17 +189,35 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
 
   if (!rows && !c.out.accumulate)
     if (ps_status r = clear_rows(c.out, t.num_keys, t.dim, st)) return r;
+  // where one workgroup sorts the ids it also gives the runs; else the rows form
+  // finds them itself, and the index of each block's first one with them
+  const bool own_runs = rows && c.n > ORDER_RUNS_MAX;
   Order o;
-  if (ps_status r = order_ids(c.ids, c.n, c.pad, t.num_keys, ws, rows, c.uniq, p.split_count, t.status, st, &o))
+  if (ps_status r = order_ids(c.ids, c.n, c.pad, t.num_keys, ws, rows && !own_runs, c.uniq, p.split_count, t.status, st,
+                              &o))
     return r;
-  const GradRuns g{o.keys, o.perm, c.n, (uint32_t)t.num_keys, rows ? o.seg_off : nullptr, o.hdr, c.num_unique,
-                   p.partial, p.block, fold_blocks(blocks), p.split_list, p.split_count};
+  if (own_runs) {
+    const int64_t tiles = div_up(c.n, RUNS_TILE);
+    const bool scan = tiles > 4096;
+    hipLaunchKernelGGL(k_runs_count, dim3(tiles), dim3(BLOCK), 0, st, o.keys, c.n, (uint32_t)t.num_keys, p.tile_heads);
+    RAISE_HIP(hipGetLastError());
+    if (scan) {
+      hipLaunchKernelGGL(k_runs_scan, dim3(1), dim3(BLOCK), 0, st, p.tile_heads, tiles);
+      RAISE_HIP(hipGetLastError());
+    }
+    hipLaunchKernelGGL(k_runs_write, dim3(tiles), dim3(BLOCK), 0, st, o.keys, c.n, (uint32_t)t.num_keys, p.tile_heads,
+                       (int)scan, p.block, c.uniq, o.seg_off, p.block_run, c.num_unique);
+    RAISE_HIP(hipGetLastError());
+  }
+  const GradRuns g{o.keys, o.perm, c.n, (uint32_t)t.num_keys, rows ? o.seg_off : nullptr, o.hdr,
+                   own_runs ? p.block_run : nullptr, c.num_unique, p.partial, p.block, fold_blocks(blocks),
+                   p.split_list, p.split_count};
   const ps_status r = with_type(c.in_type, [&]<class IT>(IT) -> ps_status {
     return with_width(vw, [&]<int VW>() -> ps_status {
       if constexpr (sizeof(IT) * VW <= 16) {
         auto kernel = p.block == 8 ? k_grad_merge<IT, VW, 8> : k_grad_merge<IT, VW, 16>;
         hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), BLOCK / lanes * sizeof(GradMeta), st, g, static_cast<const IT*>(c.dout),
-                           c.in_ld, t.dim, lanes, slices, (double)c.scale, c.out);
+                           c.in_ld, t.dim, lanes, slices, c.scale, c.out);
         RAISE_HIP(hipGetLastError());
       }
       return PS_OK;
@@ -211,7 +233,7 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
     RAISE_HIP(hipGetLastError());
   }
   hipLaunchKernelGGL(k_grad_finish, dim3(std::min<int64_t>(div_up(blocks * col_slices, WAVES_PER_BLOCK), 2048)), dim3(BLOCK), 0, st, g, t.dim,
-                     col_slices, p.fold, (double)c.scale, c.out);
+                     col_slices, p.fold, c.scale, c.out);
   RAISE_HIP(hipGetLastError());
   return PS_OK;
 }

@@ -83,27 +83,115 @@ struct GradOut {
   int32_t accumulate;
 };
 
+template <int VW>
+__device__ __forceinline__ void write_row_any(const GradOut& o, int64_t row, int col, const float* x) {
+  const int64_t at = row * o.ld + col;
+  if (o.type == 0) store_any<float, VW>(static_cast<float*>(o.p) + at, raw_make<float, VW>(x));
+  else if (o.type == 1) store_any<bf16_t, VW>(static_cast<bf16_t*>(o.p) + at, raw_make<bf16_t, VW>(x));
+  else store_any<f16_t, VW>(static_cast<f16_t*>(o.p) + at, raw_make<f16_t, VW>(x));
+}
+
 template <class OT, int VW>
-__device__ __forceinline__ void write_grad(const GradOut& o, int64_t row, int col, const double* acc, double scale) {
-  OT* p = static_cast<OT*>(o.p) + row * o.ld + col;
-  float x[VW];
-  if (o.accumulate) {
-    const raw_t<OT, VW> old = load_any<OT, VW>(p);
+__device__ __forceinline__ void add_old(const GradOut& o, int64_t at, double* x) {
+  const raw_t<OT, VW> old = load_any<OT, VW>(static_cast<const OT*>(o.p) + at);
 #pragma unroll
-    for (int e = 0; e < VW; ++e) x[e] = (float)((double)raw_get<OT, VW>(old, e) + scale * acc[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < VW; ++e) x[e] = (float)(scale * acc[e]);
-  }
-  store_any<OT, VW>(p, raw_make<OT, VW>(x));
+  for (int e = 0; e < VW; ++e) x[e] += (double)raw_get<OT, VW>(old, e);
 }
 
 template <int VW>
 __device__ __forceinline__ void write_grad_any(const GradOut& o, int64_t row, int col, const double* acc,
-                                               double scale) {
-  if (o.type == 0) write_grad<float, VW>(o, row, col, acc, scale);
-  else if (o.type == 1) write_grad<bf16_t, VW>(o, row, col, acc, scale);
-  else write_grad<f16_t, VW>(o, row, col, acc, scale);
+                                               float scale) {
+  double x[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) x[e] = (double)scale * acc[e];
+  if (o.accumulate) {
+    const int64_t at = row * o.ld + col;
+    if (o.type == 0) add_old<float, VW>(o, at, x);
+    else if (o.type == 1) add_old<bf16_t, VW>(o, at, x);
+    else add_old<f16_t, VW>(o, at, x);
+  }
+  float y[VW];
+#pragma unroll
+  for (int e = 0; e < VW; ++e) y[e] = (float)x[e];
+  write_row_any<VW>(o, row, col, y);
+}
+
+// The runs of the sorted keys, for the rows form of calls whose sort does not
+// give them: tiles of RUNS_TILE positions count the runs that start in them;
+// then every tile adds up the counts before its own and writes its runs' keys
+// and first positions, and the run that each of its blocks starts in.
+constexpr int RUNS_ITEMS = 16;
+constexpr int RUNS_TILE = BLOCK * RUNS_ITEMS;
+
+// The keys of a thread's positions and the bits of those that start a run.
+__device__ __forceinline__ uint32_t run_heads(const uint32_t* __restrict__ keys, int64_t n, uint32_t sentinel,
+                                              int64_t p, uint32_t (&k)[RUNS_ITEMS + 1]) {
+  const uint32_t before = p > 0 && p <= n ? keys[p - 1] : 0xffffffffu;
+#pragma unroll
+  for (int i = 0; i <= RUNS_ITEMS; ++i) k[i] = p + i < n ? keys[p + i] : 0xffffffffu;
+  uint32_t heads = 0;
+#pragma unroll
+  for (int i = 0; i < RUNS_ITEMS; ++i)
+    heads |= (uint32_t)(k[i] < sentinel && (i ? k[i - 1] : before) != k[i]) << i;
+  return heads;
+}
+
+__global__ __launch_bounds__(BLOCK) void k_runs_count(const uint32_t* __restrict__ keys, int64_t n, uint32_t sentinel,
+                                                      uint32_t* __restrict__ tile_heads) {
+  __shared__ uint32_t smem[WAVES_PER_BLOCK + 1];
+  uint32_t k[RUNS_ITEMS + 1], total;
+  const int64_t p = (int64_t)blockIdx.x * RUNS_TILE + threadIdx.x * RUNS_ITEMS;
+  block_exclusive_scan(__popc(run_heads(keys, n, sentinel, p, k)), smem, &total);
+  if (threadIdx.x == 0) tile_heads[blockIdx.x] = total;
+}
+
+// One workgroup: tile_heads becomes the runs before each tile (where there are
+// so many tiles that adding them up in each would take longer).
+__global__ __launch_bounds__(BLOCK) void k_runs_scan(uint32_t* __restrict__ tile_heads, int64_t tiles) {
+  __shared__ uint32_t smem[WAVES_PER_BLOCK + 1];
+  uint32_t carry = 0;
+  for (int64_t t0 = 0; t0 < tiles; t0 += BLOCK) {
+    const int64_t t = t0 + threadIdx.x;
+    uint32_t total;
+    const uint32_t before = block_exclusive_scan(t < tiles ? tile_heads[t] : 0u, smem, &total);
+    if (t < tiles) tile_heads[t] = carry + before;
+    carry += total;
+  }
+}
+
+__global__ __launch_bounds__(BLOCK) void k_runs_write(const uint32_t* __restrict__ keys, int64_t n, uint32_t sentinel,
+                                                      const uint32_t* __restrict__ tile_heads, int scanned, int block,
+                                                      int64_t* __restrict__ uniq, int32_t* __restrict__ seg_off,
+                                                      int32_t* __restrict__ block_run,
+                                                      int32_t* __restrict__ num_unique) {
+  __shared__ uint32_t smem[WAVES_PER_BLOCK + 1];
+  uint32_t before = 0, total;
+  if (scanned) {
+    before = tile_heads[blockIdx.x];
+  } else {
+    for (int t = threadIdx.x; t < (int)blockIdx.x; t += BLOCK) before += tile_heads[t];
+    block_exclusive_scan(before, smem, &total);
+    before = total;
+  }
+  uint32_t k[RUNS_ITEMS + 1];
+  const int64_t p = (int64_t)blockIdx.x * RUNS_TILE + threadIdx.x * RUNS_ITEMS;
+  const uint32_t heads = run_heads(keys, n, sentinel, p, k);
+  uint32_t u = before + block_exclusive_scan(__popc(heads), smem, &total);   // runs that start before position p + i
+#pragma unroll
+  for (int i = 0; i < RUNS_ITEMS; ++i) {
+    const bool head = (heads >> i) & 1u;
+    if ((p + i) % block == 0 && p + i < n) block_run[(p + i) / block] = (int32_t)(u + head) - 1;
+    if (head) {
+      uniq[u] = (int64_t)k[i];
+      seg_off[u] = (int32_t)(p + i);
+      ++u;
+    }
+    if (k[i] < sentinel && k[i + 1] >= sentinel) {   // the last position of the last run
+      seg_off[u] = (int32_t)(p + i) + 1;
+      *num_unique = (int32_t)u;
+    }
+  }
+  if (p == 0 && k[0] >= sentinel) *num_unique = 0;
 }
 
 // Index of the run that holds sorted position p, the last u with
@@ -131,7 +219,8 @@ struct GradRuns {
   int64_t n;
   uint32_t sentinel;
   const int32_t* seg_off;  // rows form only
-  const SegHeader* hdr;
+  const SegHeader* hdr;    // rows form, from the sort: the number of runs;
+  const int32_t* block_run;  // or, from k_runs_write, the run of each block's first position
   int32_t* num_unique;     // rows form: receives the number of rows
   double* partial;         // [2 * blocks][dim]
   int block;               // positions of a block
@@ -154,7 +243,7 @@ struct GradMeta {
 // round.
 template <class IT, int VW, int BLK>
 __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __restrict__ dout, int64_t in_ld, int dim,
-                                                      int lanes, int slices, double scale, GradOut out) {
+                                                      int lanes, int slices, float scale, GradOut out) {
   constexpr int U = BLK;
   extern __shared__ GradMeta grad_meta[];   // one per group
   const int64_t group = (int64_t)blockIdx.x * (BLOCK / lanes) + threadIdx.x / lanes;
@@ -164,7 +253,7 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
   const int at = (slice * lanes + gl) * VW;
   const bool active = at < dim;
   const int col = at + VW <= dim ? at : dim - VW;   // the last vector ends with the row, as in k_embed
-  if (g.seg_off && group == 0 && gl == 0) *g.num_unique = (int32_t)g.hdr->num_unique;
+  if (g.seg_off && !g.block_run && group == 0 && gl == 0) *g.num_unique = (int32_t)g.hdr->num_unique;
   const int64_t p0 = b * BLK;
   if (p0 >= g.n) return;
   GradMeta& m = grad_meta[threadIdx.x / lanes];
@@ -183,7 +272,9 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
                       m.key[2 * BLK] != last;                  // as this block does its own last run
   const int stop = extend ? 2 * BLK : count;
   // (before the rows are asked for: behind them its loads would wait for them)
-  int32_t u = g.seg_off ? run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)p0, lanes, gl) : 0;
+  int32_t u = 0;   // its index (rows form)
+  if (g.block_run) u = g.block_run[b];
+  else if (g.seg_off) u = run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)p0, lanes, gl);
   int start = 0;   // the run's first position here
   const IT* src = dout + col;
   double acc[VW];
@@ -204,9 +295,20 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
     for (int i = 0; i < U; ++i) {
       const uint32_t k = m.key[p + i];
       if (k >= g.sentinel || (p > 0 && k != last)) return;   // nothing of this group's follows
+      const bool ends = m.key[p + i + 1] != k;
+      if (ends && start == p + i && !came_in && !out.accumulate) {
+        // a token that comes once: its product in fp32 is the fp64 one (of two
+        // 24-bit numbers, exact) rounded
+        float y[VW];
+#pragma unroll
+        for (int e = 0; e < VW; ++e) y[e] = scale * raw_get<IT, VW>(x[i], e);
+        if (active) write_row_any<VW>(out, g.seg_off ? (int64_t)u : (int64_t)k, col, y);
+        start = p + i + 1;
+        ++u;
+        continue;
+      }
 #pragma unroll
       for (int e = 0; e < VW; ++e) acc[e] += (double)raw_get<IT, VW>(x[i], e);
-      const bool ends = m.key[p + i + 1] != k;
       const bool leaves = !ends && p + i + 1 == count && !extend;
       if (!ends && !leaves) continue;
       if (taken && k == first) {
@@ -275,22 +377,17 @@ __global__ __launch_bounds__(BLOCK) void k_grad_fold(GradRuns g, int64_t supers,
   }
 }
 
-// The last block that the run of `key`, which comes into block f, comes into;
-// most runs are short, so the steps double from there on.
+// The last block that the run of `key`, which comes into block f, comes into,
+// by the wave's lanes together as in run_at.
 __device__ __forceinline__ int64_t last_block(const GradRuns& g, uint32_t key, int64_t f) {
   const int64_t blocks = (g.n + g.block - 1) / g.block;
-  int64_t lo = f, hi = blocks;   // it comes into lo, not into hi
-  for (int64_t step = 1; lo + step < blocks; step *= 2) {
-    if (g.keys[(lo + step) * g.block] != key) {
-      hi = lo + step;
-      break;
-    }
-    lo += step;
-  }
-  while (hi - lo > 1) {
-    const int64_t mid = lo + (hi - lo) / 2;
-    if (g.keys[mid * g.block] == key) lo = mid;
-    else hi = mid;
+  int64_t lo = f, len = blocks - f;   // it comes into lo, not into lo + len
+  while (len > 1) {
+    const int64_t step = (len + WAVE - 1) / WAVE;
+    const int64_t at = (lane_id() + 1) * step;
+    const int k = __popcll(__ballot(at < len && g.keys[(lo + at) * g.block] == key));
+    lo += k * step;
+    len = len - k * step < step ? len - k * step : step;
   }
   return lo;
 }
@@ -299,7 +396,7 @@ __device__ __forceinline__ int64_t last_block(const GradRuns& g, uint32_t key, i
 // to the first folded ones, the folds, and the blocks after them, added in
 // this order.
 __global__ __launch_bounds__(BLOCK) void k_grad_finish(GradRuns g, int dim, int slices,
-                                                       const double* __restrict__ fold, double scale, GradOut out) {
+                                                       const double* __restrict__ fold, float scale, GradOut out) {
   const int64_t items = (int64_t)*g.split_count * slices;
   const int64_t step = (int64_t)gridDim.x * WAVES_PER_BLOCK;
   for (int64_t e = (int64_t)blockIdx.x * WAVES_PER_BLOCK + threadIdx.x / WAVE; e < items; e += step) {
@@ -308,7 +405,8 @@ __global__ __launch_bounds__(BLOCK) void k_grad_finish(GradRuns g, int dim, int 
     const int4 run = g.split_list[r];
     const int64_t s0 = run.x;
     const uint32_t key = (uint32_t)run.y;
-    const int64_t f = s0 / g.block + 1, l = last_block(g, key, f);   // the blocks it comes into
+    const int64_t f = s0 / g.block + 1;   // the blocks it comes into: f to l
+    const int64_t l = g.seg_off ? (g.seg_off[run.z + 1] - 1) / g.block : last_block(g, key, f);
     const int64_t sa = (f + g.fold - 1) / g.fold, sb = (l + 1) / g.fold;
     const int64_t nf = sb > sa ? sb - sa : 0;
     const int64_t n1 = nf ? sa * g.fold - f : l - f + 1;

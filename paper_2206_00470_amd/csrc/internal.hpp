@@ -39,14 +39,17 @@ ADAPM_HIDDEN TableView table_view(const ps_store* s);
 
 // A stable sort of n ids in [0, num_keys): sorted keys (num_keys marks the
 // ids that take no part: `pad` silently, others outside the range with
-// *err raised), the occurrence of each sorted position, and, where asked for,
-// the runs of equal keys: their distinct keys in uniq, their first positions
-// in seg_off (seg_off[U] = ids that take part), U in hdr->num_unique.
+// *err raised) and the occurrence of each sorted position.  With `runs` (n up to
+// ORDER_RUNS_MAX) also the runs of equal keys: their distinct keys in uniq,
+// their first positions in seg_off (seg_off[U] = ids that take part), U in
+// hdr->num_unique; else seg_off is room for n + 1 positions.
 // *counter, if given, is set to zero.
+constexpr int64_t ORDER_RUNS_MAX = 8192;
+
 struct Order {
   const uint32_t* keys;
   const uint32_t* perm;
-  const int32_t* seg_off;
+  int32_t* seg_off;
   const SegHeader* hdr;
 };
 

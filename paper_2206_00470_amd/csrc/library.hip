@@ -51,12 +51,14 @@ ps_status order_ids(const int64_t* ids, int64_t n, int64_t pad, int64_t num_keys
   Carver c(ws);
   carve_sort(c, n, 1, false, true, &b);
   uint32_t *ks, *perm;
-  if (!runs && n > SMALL_KEYS_MAX) {
+  static_assert(ORDER_RUNS_MAX == SMALL_KEYS_MAX, "one workgroup gives the runs with the sort");
+  if (n > SMALL_KEYS_MAX) {
+    if (runs) return fail(PS_ERR_UNSUPPORTED, "runs of %lld ids", (long long)n);
     // the sort alone: run_keywork's without its last kernels
     const KeysPadded keys{ids, pad, counter};
     if (n > MID_KEYS_MAX) {
       if (ps_status r = run_sort(nullptr, keys, n, num_keys, b, err, nullptr, false, st, &ks, &perm)) return r;
-      *out = Order{ks, perm, nullptr, nullptr};
+      *out = Order{ks, perm, b.seg_off, nullptr};
       return PS_OK;
     }
     const RadixPlan plan = radix_plan(num_keys);
@@ -75,7 +77,7 @@ ps_status order_ids(const int64_t* ids, int64_t n, int64_t pad, int64_t num_keys
                          b.k[1 - p % 2], b.v[1 - p % 2], nullptr);
       LAUNCHED(k_mid_scatter);
     }
-    *out = Order{b.k[plan.passes % 2], b.v[plan.passes % 2], nullptr, nullptr};
+    *out = Order{b.k[plan.passes % 2], b.v[plan.passes % 2], b.seg_off, nullptr};
     return PS_OK;
   }
   if (ps_status r = run_keywork(nullptr, KeysPadded{ids, pad, counter}, n, num_keys, b, err, nullptr, false, st, &ks,

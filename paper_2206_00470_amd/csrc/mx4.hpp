@@ -159,15 +159,15 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__
 // The codes are staged in LDS eight blocks of a row at a time, copied there
 // without a detour through registers: read straight from memory, the fragments
 // of one instruction lie in 32 lines (2,048 x 131,072 of dim 512 326 us against
-// 153). One buffer: other workgroups of the compute unit fill the wait better
-// than a second buffer does (200 us), since that leaves room for two of them
-// instead of three.
+// 136). One buffer: other workgroups of the compute unit fill the wait better
+// than a second buffer does, which leaves room for two of them instead of four
+// (200 us; with registers for three 146).
 //
 // Bound by C's bytes where there are many queries (a table's width is a few
 // hundred: 2 dim operations per element written), by B's where there are few.
 // Measured: one query x 4.6M rows of 256 108 us, 6.0 TB/s of rows read and
 // scores written; 2,048 x 131,072 of dim 64 in bf16 99 us, 5.5 TB/s, of dim 512
-// 153 us, 3.7 TB/s and 1,800 TFLOP/s; 2,048 x 31,000 of dim 2,048 130 us, 2,000
+// 136 us, 4.2 TB/s and 2,000 TFLOP/s; 2,048 x 31,000 of dim 2,048 117 us, 2,200
 // TFLOP/s.
 typedef int mx_operand __attribute__((ext_vector_type(8)));
 typedef float mx_acc __attribute__((ext_vector_type(16)));
@@ -178,36 +178,49 @@ struct MxRows {
   int64_t rows;
 };
 
+// A workgroup's rows of one operand: the first row's codes and scales, and the
+// last row there is (rows beyond it are read as it, and not stored).  Offsets
+// inside a tile are 32 bits.
+struct MxTile {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int last;
+};
+
+__device__ __forceinline__ MxTile mx_rows(const MxRows& t, int64_t row0, int rows, int blocks_row) {
+  const int64_t left = t.rows - 1 - row0;
+  return MxTile{t.codes + row0 * blocks_row * MX_BYTES, t.scales + row0 * blocks_row,
+                left < rows - 1 ? (int)left : rows - 1};
+}
+
 // Staged codes: rows of eight blocks (128 bytes), block b of a row in slot
 // b ^ (row / 2 % 8), so that the blocks of one number of sixteen rows lie in
 // sixteen different slots of 256 bytes: reading them has no bank conflict.
 __device__ __forceinline__ int mx_slot(int row, int b) { return row * 8 + (b ^ ((row >> 1) & 7)); }
 
-// Copies blocks k0 .. k0+7 of the ROWS rows from row0 on into LDS, the eight
-// rows of an instruction side by side.  Rows beyond the last are taken from the
-// last, blocks beyond the row's end from its last block.
+// Copies blocks k0 .. k0+7 of the tile's ROWS rows into LDS, the eight rows of
+// an instruction side by side.  Blocks beyond a row's end are taken from its
+// last block.
 template <int ROWS>
-__device__ __forceinline__ void mx_stage(const MxRows& t, int64_t row0, int k0, int blocks_row, words4* to) {
+__device__ __forceinline__ void mx_stage(const MxTile& t, int k0, int blocks_row, words4* to) {
   const int w = threadIdx.x / WAVE, l = lane_id();
+  // (the rows of one thread are 32 apart: their blocks have the same slots)
+  const int kb = k0 + ((l % 8) ^ (((w * 8 + l / 8) >> 1) & 7));
+  const uint32_t at = (kb < blocks_row ? kb : blocks_row - 1) * MX_BYTES;
 #pragma unroll
   for (int i = 0; i < ROWS / 8; i += WAVES_PER_BLOCK) {
-    const int g = i + w;   // (ROWS / 8 is a multiple of the number of waves)
-    const int rt = g * 8 + l / 8;
-    int64_t row = row0 + rt;
-    if (row >= t.rows) row = t.rows - 1;
-    int kb = k0 + ((l % 8) ^ ((rt >> 1) & 7));
-    if (kb >= blocks_row) kb = blocks_row - 1;
-    const uint8_t* src = t.codes + (row * blocks_row + kb) * MX_BYTES;
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                     (__attribute__((address_space(3))) void*)(to + g * WAVE), 16, 0, 0);
+    const int row = (i + w) * 8 + l / 8;   // (ROWS / 8 is a multiple of the number of waves)
+    const uint32_t off = (uint32_t)(row < t.last ? row : t.last) * (uint32_t)(blocks_row * MX_BYTES) + at;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(t.codes + off),
+                                     (__attribute__((address_space(3))) void*)(to + (i + w) * WAVE), 16, 0, 0);
   }
 }
 
 // The scale bytes of blocks kb .. kb+count-1 of a row (count at most 4), 1
 // where they are beyond its end.
 template <bool FULL>
-__device__ __forceinline__ uint32_t mx_scales(const MxRows& t, int64_t row, int kb, int count, int blocks_row) {
-  const uint8_t* p = t.scales + row * blocks_row + kb;
+__device__ __forceinline__ uint32_t mx_scales(const MxTile& t, int row, int kb, int count, int blocks_row) {
+  const uint8_t* p = t.scales + (uint32_t)((row < t.last ? row : t.last) * blocks_row + kb);
   uint32_t s;
   if constexpr (FULL) {
     __builtin_memcpy(&s, p, 4);
@@ -251,7 +264,7 @@ __device__ __forceinline__ void mx_tile(int64_t tiles_q, int64_t tiles_b, int64_
 // A wave's tile is QT x 32 rows of A by TT x 32 rows of B; a workgroup's waves
 // stand WQ x WT.  Rows of C are stored 16 bytes at a time wherever they start.
 template <class OT, int QT, int TT, int WQ, int WT, bool NT>
-__global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int blocks_row, float scale,
+__global__ __launch_bounds__(BLOCK, 4) void k_mx4_product(MxRows A, MxRows B, int blocks_row, float scale,
                                                        OT* __restrict__ C, int64_t ldc, int64_t tiles_q) {
   constexpr int VW = 16 / sizeof(OT);
   constexpr int ET = sizeof(OT) == 2 && TT % 4 == 0 ? 4 : 2;   // tiles that leave together: rows of 256 or 128 bytes
@@ -268,11 +281,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int b
   const int64_t i0 = tq * RA + wa, j0 = tb * RB + wb;
   const int half = l / 32, r = l % 32;
   words4 *sa = lds, *sb = lds + RA * 8;
-  int64_t ra[QT], rb[TT];   // the lane's rows
-#pragma unroll
-  for (int q = 0; q < QT; ++q) ra[q] = i0 + q * 32 + r < A.rows ? i0 + q * 32 + r : A.rows - 1;
-#pragma unroll
-  for (int t = 0; t < TT; ++t) rb[t] = j0 + t * 32 + r < B.rows ? j0 + t * 32 + r : B.rows - 1;
+  const MxTile ta = mx_rows(A, tq * RA, RA, blocks_row), tbl = mx_rows(B, tb * RB, RB, blocks_row);
   mx_acc acc[QT][TT];
 #pragma unroll
   for (int q = 0; q < QT; ++q)
@@ -301,8 +310,8 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int b
   };
   auto stage = [&](int k0) {
     if (k0 > 0) __syncthreads();
-    mx_stage<RB>(B, tb * RB, k0, blocks_row, sb);
-    mx_stage<RA>(A, tq * RA, k0, blocks_row, sa);
+    mx_stage<RB>(tbl, k0, blocks_row, sb);
+    mx_stage<RA>(ta, k0, blocks_row, sa);
   };
   auto staged = [&] {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -312,9 +321,9 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int b
   for (; k0 + 8 <= blocks_row; k0 += 8) {
     stage(k0);
 #pragma unroll
-    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<true>(B, rb[t], k0 + 4 * half, 4, blocks_row);
+    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<true>(tbl, wb + t * 32 + r, k0 + 4 * half, 4, blocks_row);
 #pragma unroll
-    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<true>(A, ra[q], k0 + 4 * half, 4, blocks_row);
+    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<true>(ta, wa + q * 32 + r, k0 + 4 * half, 4, blocks_row);
     staged();
     multiply.template operator()<0, true>(4 * half, 8);
     multiply.template operator()<1, true>(4 * half, 8);
@@ -325,9 +334,9 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_product(MxRows A, MxRows B, int b
     const int rem = blocks_row - k0, per = (rem + 1) / 2;
     stage(k0);
 #pragma unroll
-    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<false>(B, rb[t], k0 + per * half, per, blocks_row);
+    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<false>(tbl, wb + t * 32 + r, k0 + per * half, per, blocks_row);
 #pragma unroll
-    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<false>(A, ra[q], k0 + per * half, per, blocks_row);
+    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<false>(ta, wa + q * 32 + r, k0 + per * half, per, blocks_row);
     staged();
     multiply.template operator()<0, false>(per * half, rem);
     if (per > 1) multiply.template operator()<1, false>(per * half, rem);
