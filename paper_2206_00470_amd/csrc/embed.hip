@@ -180,11 +180,11 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
   auto fits = [&](int w) { return apart ? t.dim % w == 0 : t.dim >= w; };
   const int vw = ib + ob == 4 && fits(8) ? 8 : fits(4) ? 4 : 1;
   const int vectors = (int)div_up(t.dim, vw);
-  int lanes = 4;
-  while (lanes < WAVE && lanes < vectors) lanes *= 2;
-  const int slices = (int)div_up(vectors, lanes);
+  int log_lanes = 2;
+  while ((1 << log_lanes) < WAVE && (1 << log_lanes) < vectors) ++log_lanes;
+  const int slices = (int)div_up(vectors, 1 << log_lanes);
   const int64_t blocks = div_up(c.n, p.block);
-  const int64_t grid = div_up(blocks * slices, BLOCK / lanes);
+  const int64_t grid = div_up(blocks, BLOCK >> log_lanes);
   if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld ids of %d exceed the merge's grid", (long long)c.n, t.dim);
 
   if (!rows && !c.out.accumulate)
@@ -216,8 +216,8 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
     return with_width(vw, [&]<int VW>() -> ps_status {
       if constexpr (sizeof(IT) * VW <= 16) {
         auto kernel = p.block == 8 ? k_grad_merge<IT, VW, 8> : k_grad_merge<IT, VW, 16>;
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), BLOCK / lanes * sizeof(GradMeta), st, g, static_cast<const IT*>(c.dout),
-                           c.in_ld, t.dim, lanes, slices, c.scale, c.out);
+        hipLaunchKernelGGL(kernel, dim3(grid, slices), dim3(BLOCK), (BLOCK >> log_lanes) * sizeof(GradMeta), st, g, static_cast<const IT*>(c.dout),
+                           c.in_ld, t.dim, log_lanes, c.scale, c.out);
         RAISE_HIP(hipGetLastError());
       }
       return PS_OK;

@@ -231,7 +231,7 @@ struct GradRuns {
 
 // Keys and occurrences of a group's positions: its block, the one after and
 // the key behind them.
-struct GradMeta {
+struct alignas(16) GradMeta {
   uint32_t key[2 * GRAD_BLOCK_MAX + 4];
   uint32_t occ[2 * GRAD_BLOCK_MAX];
 };
@@ -243,66 +243,75 @@ struct GradMeta {
 // round.
 template <class IT, int VW, int BLK>
 __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __restrict__ dout, int64_t in_ld, int dim,
-                                                      int lanes, int slices, float scale, GradOut out) {
+                                                      int log_lanes, float scale, GradOut out) {
   constexpr int U = BLK;
   extern __shared__ GradMeta grad_meta[];   // one per group
-  const int64_t group = (int64_t)blockIdx.x * (BLOCK / lanes) + threadIdx.x / lanes;
+  const int lanes = 1 << log_lanes;
   const int gl = threadIdx.x & (lanes - 1);
-  const int64_t b = group / slices;
-  const int slice = (int)(group - b * slices);
+  const int64_t b = (int64_t)blockIdx.x * (BLOCK >> log_lanes) + (threadIdx.x >> log_lanes);
+  const int slice = blockIdx.y;
   const int at = (slice * lanes + gl) * VW;
   const bool active = at < dim;
   const int col = at + VW <= dim ? at : dim - VW;   // the last vector ends with the row, as in k_embed
-  if (g.seg_off && !g.block_run && group == 0 && gl == 0) *g.num_unique = (int32_t)g.hdr->num_unique;
   const int64_t p0 = b * BLK;
   if (p0 >= g.n) return;
-  GradMeta& m = grad_meta[threadIdx.x / lanes];
-  for (int i = gl; i <= 2 * BLK; i += lanes) m.key[i] = p0 + i < g.n ? g.keys[p0 + i] : 0xffffffffu;
-  for (int i = gl; i < 2 * BLK; i += lanes) m.occ[i] = p0 + i < g.n ? g.perm[p0 + i] : 0u;
   const uint32_t before = p0 > 0 ? g.keys[p0 - 1] : 0xffffffffu;
   const uint32_t before2 = p0 > BLK ? g.keys[p0 - BLK - 1] : 0xffffffffu;
+  int32_t u = g.block_run ? g.block_run[b] : 0;   // the run's index (rows form)
+  GradMeta& m = grad_meta[threadIdx.x >> log_lanes];
+  for (int i = gl; i <= 2 * BLK; i += lanes) m.key[i] = p0 + i < g.n ? g.keys[p0 + i] : 0xffffffffu;
+  for (int i = gl; i < 2 * BLK; i += lanes) m.occ[i] = p0 + i < g.n ? g.perm[p0 + i] : 0u;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // a group's lanes are of one wave
   __builtin_amdgcn_wave_barrier();
   const int count = g.n - p0 < BLK ? (int)(g.n - p0) : BLK;
   const uint32_t first = m.key[0], last = m.key[count - 1], next = m.key[count];
+  if (g.seg_off && !g.block_run) {
+    if (b == 0 && slice == 0 && gl == 0) *g.num_unique = (int32_t)g.hdr->num_unique;
+    // (before the rows are asked for: behind them its loads would wait for them)
+    u = run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)p0, lanes, gl);
+  }
   if (first >= g.sentinel) return;
   bool came_in = before == first;                                     // the run began in an earlier block
   const bool taken = came_in && before2 != first && next != first;    // which takes it whole
   const bool extend = count == BLK && next == last && !(came_in && last == first) &&
-                      m.key[2 * BLK] != last;                  // as this block does its own last run
+                      m.key[2 * BLK] != last;                         // as this block does its own last run
   const int stop = extend ? 2 * BLK : count;
-  // (before the rows are asked for: behind them its loads would wait for them)
-  int32_t u = 0;   // its index (rows form)
-  if (g.block_run) u = g.block_run[b];
-  else if (g.seg_off) u = run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)p0, lanes, gl);
   int start = 0;   // the run's first position here
   const IT* src = dout + col;
   double acc[VW];
 #pragma unroll
   for (int e = 0; e < VW; ++e) acc[e] = 0.0;
   for (int p = 0; p < stop; p += U) {
+    uint32_t k[U + 1], r[U];
+#pragma unroll
+    for (int i = 0; i < U; i += 4) {
+      const words4 a = *reinterpret_cast<const words4*>(m.key + p + i);
+      const words4 c = *reinterpret_cast<const words4*>(m.occ + p + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[i + e] = a[e], r[i + e] = c[e];
+    }
+    k[U] = m.key[p + U];
+    // every position's row, its own or not: an occurrence is a row of dout
+    // (the first one stands for those beyond the last)
     raw_t<IT, VW> x[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      x[i] = raw_t<IT, VW>{};
-      const uint32_t k = m.key[p + i];
-      if (active && k < g.sentinel && !(taken && k == first) && (p == 0 || k == last))
-        x[i] = load_any<IT, VW>(src + (int64_t)m.occ[p + i] * in_ld);
-    }
+    for (int i = 0; i < U; ++i) x[i] = load_any<IT, VW>(src + (int64_t)r[i] * in_ld);
+    int mine = 0;   // positions that are this group's: the first of them
+#pragma unroll
+    for (int i = 0; i < U; ++i) mine += k[i] < g.sentinel && (p == 0 || k[i] == last) ? 1 : 0;
 #pragma unroll
     for (int i = 0; i < U; ++i) asm volatile("" : "+v"(x[i]));
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const uint32_t k = m.key[p + i];
-      if (k >= g.sentinel || (p > 0 && k != last)) return;   // nothing of this group's follows
-      const bool ends = m.key[p + i + 1] != k;
+      if (i >= mine) return;   // nothing of this group's follows
+      const bool ends = k[i + 1] != k[i];
       if (ends && start == p + i && !came_in && !out.accumulate) {
         // a token that comes once: its product in fp32 is the fp64 one (of two
         // 24-bit numbers, exact) rounded
         float y[VW];
 #pragma unroll
         for (int e = 0; e < VW; ++e) y[e] = scale * raw_get<IT, VW>(x[i], e);
-        if (active) write_row_any<VW>(out, g.seg_off ? (int64_t)u : (int64_t)k, col, y);
+        if (active) write_row_any<VW>(out, g.seg_off ? (int64_t)u : (int64_t)k[i], col, y);
         start = p + i + 1;
         ++u;
         continue;
@@ -311,9 +320,9 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
       for (int e = 0; e < VW; ++e) acc[e] += (double)raw_get<IT, VW>(x[i], e);
       const bool leaves = !ends && p + i + 1 == count && !extend;
       if (!ends && !leaves) continue;
-      if (taken && k == first) {
+      if (taken && k[i] == first) {
       } else if (ends && !came_in) {
-        if (active) write_grad_any<VW>(out, g.seg_off ? (int64_t)u : (int64_t)k, col, acc, scale);
+        if (active) write_grad_any<VW>(out, g.seg_off ? (int64_t)u : (int64_t)k[i], col, acc, scale);
       } else {
         if (active) {
           double* q = g.partial + (2 * b + (start != 0 ? 1 : 0)) * dim + col;
@@ -321,7 +330,7 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
           for (int e = 0; e < VW; ++e) q[e] = acc[e];
         }
         if (leaves && !came_in && gl == 0 && slice == 0)
-          g.split_list[atomicAdd(g.split_count, 1u)] = int4{(int)p0 + start, (int)k, u, 0};
+          g.split_list[atomicAdd(g.split_count, 1u)] = int4{(int)p0 + start, (int)k[i], u, 0};
       }
 #pragma unroll
       for (int e = 0; e < VW; ++e) acc[e] = 0.0;
