@@ -108,9 +108,13 @@ class MX4:
             raise ValueError(f"rows of {dim} values have {16 * nb} bytes of codes and {nb} scales")
         if codes.device != scales.device:
             raise TypeError("codes and scales must be on one device")
+        self._set(codes, scales, dim)
+
+    def _set(self, codes, scales, dim):
         self.codes, self.scales, self.dim = codes, scales, dim
         self.rows, self.device = codes.shape[0], codes.device
         self._err = None
+        return self
 
     def embed(self, ids: torch.Tensor, scale: float = 1.0, dtype: torch.dtype = torch.float32, pad: int | None = None,
               out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
@@ -162,7 +166,7 @@ def mx4_quantize(x: torch.Tensor, stream=None) -> MX4:
         codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=x.device)
         scales = torch.empty((rows, nb), dtype=torch.uint8, device=x.device)
         check(lib().ps_mx4_quantize(rows, dim, _type(x.dtype, "x"), _ptr(x), ld, _ptr(codes), _ptr(scales), st))
-    return MX4(codes, scales, dim)
+    return MX4.__new__(MX4)._set(codes, scales, dim)
 
 
 def mx4_product(a: MX4, b: MX4, scale: float = 1.0, dtype: torch.dtype = torch.float32,

@@ -344,12 +344,14 @@ class Store:
             n, ld, kind, ws = self._grad_args(ids, dout)
             uniq = torch.empty(n, dtype=torch.int64, device=self.W.device)
             rows = torch.empty((n, self.dim), dtype=dtype, device=self.W.device)
-            # (an address even where there are no ids)
-            count = torch.empty(1, dtype=torch.int32, device=self.W.device)
+            # the number comes straight to host memory: no copy to wait for behind the kernels
+            count = torch.empty(1, dtype=torch.int32, pin_memory=True)
+            # (rows: an address even where there are no ids)
             check(lib().ps_embed_grad_rows(self._h, _ptr(ids), n, _pad(pad), scale, kind, _ptr(dout), ld,
-                                           _type(dtype, "dtype"), _ptr(uniq), _ptr(rows) if n else _ptr(count),
-                                           self.dim, _ptr(count), _ptr(ws), ws.numel(), st))
-            U = int(count.item())
+                                           _type(dtype, "dtype"), _ptr(uniq), _ptr(rows if n else count), self.dim,
+                                           _ptr(count), _ptr(ws), ws.numel(), st))
+            torch.cuda.current_stream(self.W.device).synchronize()
+            U = int(count)
         return uniq[:U], rows[:U]
 
     # ---------------------------------------------------------------- task steps

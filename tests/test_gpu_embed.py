@@ -216,6 +216,59 @@ def test_embed_grad_matches_sums_in_64_bits(K, d, n, kind, form):
     assert not W.cpu().numpy().any()
 
 
+# both sides of the lines between the kernels: one workgroup's sort and the tiled ones, blocks of 8
+# and of 16, none, 16 and 64 blocks folded together, tiles' counts added up in each and scanned
+LINES = [(600, 4, 8192, "zipf"), (600, 4, 8193, "zipf"), (50, 7, 8193, "same"), (3000, 2048, 8191, "zipf"),
+         (3000, 2048, 8192, "zipf"), (3000, 2048, 8193, "zipf"), (30, 64, 2048, "same"), (30, 64, 2056, "same"), (30, 64, 2057, "zipf"),
+         (5, 80, 262_144, "same"), (7, 80, 300_000, "zipf"), (100_000, 5, 393_217, "zipf"),
+         (3_000_000, 4, 16_777_216, "zipf"), (3_000_000, 4, 16_785_413, "zipf")]
+
+
+@pytest.mark.parametrize("form", ["dense", "rows"])
+@pytest.mark.parametrize("K,d,n,kind", LINES)
+def test_embed_grad_on_both_sides_of_its_lines(K, d, n, kind, form):
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    ids = make_ids(K, n, 140 + d, kind)
+    dout = torch.randn((n, d), generator=torch.Generator().manual_seed(141 + d)).to(BF16)
+    say(f"grad {form} K={K} d={d} n={n} {kind}")
+    ref, mag, count = plain_grad(K, ids, dout, 1.0, None)
+    if form == "dense":
+        check_grad(s.embed_grad(ids.cuda(), dout.cuda()), ref, mag, count, F32)
+    else:
+        uniq, rows = s.embed_grad_rows(ids.cuda(), dout.cuda())
+        want = torch.nonzero(count)[:, 0]
+        assert torch.equal(uniq.cpu(), want)
+        check_grad(rows, ref[want], mag[want], count[want], F32)
+    assert s.error() == 0
+
+
+@pytest.mark.parametrize("runs", [[15, 1, 17, 31, 1, 16, 2, 33, 48, 1], [16, 16, 16, 32, 32], [1] * 40 + [47, 49, 1],
+                                  [8, 8, 24, 8, 9, 7, 16], [31, 33, 64, 5, 100, 3, 29]])
+def test_embed_grad_runs_against_block_ends(runs):
+    """Runs that start and end on, before and after the ends of blocks."""
+    d = 20
+    K = len(runs) + 3
+    s = Store(torch.zeros((K, d), device="cuda"), torch.ones((K, d), device="cuda"))
+    ids = torch.repeat_interleave(torch.arange(len(runs)), torch.tensor(runs))
+    for at in range(0, 40, 3):   # the same runs behind `at` other ids
+        shifted = torch.cat([torch.zeros(at, dtype=torch.int64), ids + 1])
+        for n in (shifted.numel(), 900_000 if at == 0 else 0):   # blocks of 8, and of 16
+            if n == 0:
+                continue
+            full = torch.cat([shifted, torch.full((n - shifted.numel(),), -1, dtype=torch.int64)])
+            order = torch.randperm(n, generator=torch.Generator().manual_seed(at))
+            full = full[order]
+            dout = torch.randn((n, d), generator=torch.Generator().manual_seed(at + 1))
+            ref, mag, count = plain_grad(K, full, dout, 1.0, -1)
+            check_grad(s.embed_grad(full.cuda(), dout.cuda(), pad=-1), ref, mag, count, F32)
+            uniq, rows = s.embed_grad_rows(full.cuda(), dout.cuda(), pad=-1)
+            want = torch.nonzero(count)[:, 0]
+            assert torch.equal(uniq.cpu(), want)
+            check_grad(rows, ref[want], mag[want], count[want], F32)
+    assert s.error() == 0
+
+
 @pytest.mark.parametrize("gout", [F32, BF16])
 @pytest.mark.parametrize("K,d,n,kind", [(50, 3, 40, "zipf"), (3000, 100, 5000, "zipf"), (64, 768, 4097, "same")])
 def test_embed_grad_accumulates(K, d, n, kind, gout):
