@@ -458,7 +458,8 @@ ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t
  *   coef = max_norm / *norm (in fp64, rounded to fp32) if *norm > max_norm,
  *   else 1.
  * Squares and sums are fp64 in a fixed order.  A norm that is NaN makes every
- * output NaN; an infinite one makes coef 0 (so the infinite elements NaN).
+ * output NaN; an infinite one above max_norm makes coef 0 (so the infinite
+ * elements NaN).
  * grads, outs, numel, types: host arrays, read during the call only, of
  * device addresses, elements and element types (PS_F32, ...); the tensors
  * are dense, of any size (0 too) and alignment.  outs[k] may be grads[k] (in
@@ -497,7 +498,8 @@ ps_status ps_mx4_embed(const uint8_t* codes, const uint8_t* scales, int64_t num_
 /* Scores of m quantised queries against n quantised rows of the same dim:
  *   out[i*out_stride + j] = T( scale * sum_k a[i][k] b[j][k] )
  * Products are exact, sums fp32 on the matrix cores (in an order that depends
- * on dim only).  out: device, out_stride >= n. */
+ * on dim only).  Codes behind a row whose dim is no multiple of 32 must be
+ * zero, as quantisation leaves them.  out: device, out_stride >= n. */
 ps_status ps_mx4_product(int64_t m, int64_t n, int32_t dim, const uint8_t* a_codes, const uint8_t* a_scales,
                          const uint8_t* b_codes, const uint8_t* b_scales, float scale, int32_t out_type, void* out,
                          int64_t out_stride, void* stream);

@@ -2,7 +2,6 @@
 #include "embed.hpp"
 
 #include <algorithm>
-#include <climits>
 
 #include "internal.hpp"
 #include "rules.hpp"
@@ -49,7 +48,7 @@ ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, floa
   const int vw = t.dim >= 8 && ob == 2 ? 8 : t.dim >= 4 ? 4 : 1;
   const SmallDiv nv = small_div((uint32_t)div_up(t.dim, vw));
   const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * EMBED_FLIGHT);
-  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the lookup's grid", (long long)n, t.dim);
+  if (grid > GRID_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the lookup's grid", (long long)n, t.dim);
   const LookupIds l{ids, n, pad, t.num_keys, t.map, t.map_keys, t.status};
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {
     return with_width(vw, [&]<int VW>() -> ps_status {
@@ -190,7 +189,7 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
   const int slices = (int)div_up(vectors, 1 << log_lanes);
   const int64_t blocks = div_up(c.n, p.block);
   const int64_t grid = div_up(blocks, BLOCK >> log_lanes);
-  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld ids of %d exceed the merge's grid", (long long)c.n, t.dim);
+  if (grid > GRID_MAX || div_up(c.n, BLOCK) > GRID_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld ids of %d exceed the merge's grid", (long long)c.n, t.dim);
 
   if (!rows && !c.out.accumulate)
     if (ps_status r = clear_rows(c.out, t.num_keys, t.dim, st)) return r;

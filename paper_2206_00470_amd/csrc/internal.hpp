@@ -60,6 +60,10 @@ ADAPM_HIDDEN ps_status order_ids(const int64_t* ids, int64_t n, int64_t pad, int
 // Largest number of occurrences of one call.
 constexpr int64_t OCC_MAX = (int64_t(1) << 31) - (int64_t(1) << 20);
 
+// Largest grid of workgroups of BLOCK threads (a launch counts its threads in 32
+// bits).
+constexpr int64_t GRID_MAX = (int64_t(1) << 32) / BLOCK - 1;
+
 inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool on_bytes(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 

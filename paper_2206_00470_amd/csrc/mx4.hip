@@ -2,7 +2,6 @@
 #include "mx4.hpp"
 
 #include <algorithm>
-#include <climits>
 
 #include "internal.hpp"
 #include "lookup.hpp"
@@ -44,7 +43,7 @@ ps_status ps_mx4_quantize(int64_t rows, int32_t dim, int32_t type, const void* x
   const SmallDiv per_row = small_div((uint32_t)blocks_of(dim) * 4);
   if (rows > INT64_MAX / (4 * per_row.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)rows);
   const int64_t grid = div_up(rows * per_row.d, BLOCK);
-  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)rows, dim);
+  if (grid > GRID_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)rows, dim);
   return with_type(type, [&]<class T>(T) -> ps_status {
     auto kernel = rows * per_row.d * 4 > LOOKUP_STREAMS ? k_mx4_quantize<T, true> : k_mx4_quantize<T, false>;
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, static_cast<hipStream_t>(stream),
@@ -73,7 +72,7 @@ ps_status ps_mx4_embed(const uint8_t* codes, const uint8_t* scales, int64_t num_
   const SmallDiv nv = small_div((uint32_t)div_up(dim, 16 / b));
   if (n > INT64_MAX / (4 * nv.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)n);
   const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * MX4_FLIGHT);
-  if (grid > INT_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)n, dim);
+  if (grid > GRID_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)n, dim);
   const LookupIds l{ids, n, pad, num_rows, nullptr, 0, err};
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {
     auto launch = [&](auto kernel) {
@@ -106,7 +105,7 @@ ps_status ps_mx4_product(int64_t m, int64_t n, int32_t dim, const uint8_t* a_cod
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {
     auto launch = [&](auto kernel, int tile_q, int tile_t) -> ps_status {
       const int64_t tq = div_up(m, tile_q), tt = div_up(n, tile_t);
-      if (tq > (INT_MAX - NUM_XCD) / tt) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld exceed the grid", (long long)m, (long long)n);
+      if (tq > (GRID_MAX - NUM_XCD) / tt) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld exceed the grid", (long long)m, (long long)n);
       hipLaunchKernelGGL(kernel, dim3(div_up(tq * tt, NUM_XCD) * NUM_XCD), dim3(BLOCK), 0,
                          static_cast<hipStream_t>(stream), A, B, blocks_of(dim),
                          scale, static_cast<OT*>(out), out_stride, tq);

@@ -62,7 +62,7 @@ class ClipPlan:
 
     def norm(self, stream=None) -> torch.Tensor:
         """The global norm of the gradients, float64[1]."""
-        with _On(self.device, stream) as st:
+        with _On(self.device, stream, self.grads) as st:
             norm, ws, wsb = self._buffers()
             check(lib().ps_grad_norm(self._n, self._in, self._numel, self._types, _ptr(norm), ws, wsb, st))
         return norm
@@ -70,7 +70,7 @@ class ClipPlan:
     def clip(self, max_norm: float, stream=None) -> torch.Tensor:
         """Write the gradients, scaled by max_norm / norm where the norm is
         larger, to the outputs; returns the norm before, float64[1]."""
-        with _On(self.device, stream) as st:
+        with _On(self.device, stream, (*self.grads, *self.out) if stream is not None else ()) as st:
             norm, ws, wsb = self._buffers()
             check(lib().ps_clip_grads(self._n, self._in, self._out, self._numel, self._types, max_norm, _ptr(norm), ws,
                                       wsb, st))
@@ -96,7 +96,8 @@ class MX4:
     """Rows of dim values in microscaled 4-bit floating point: codes
     uint8[rows, ceil(dim/32)*16] (two to a byte, the first in the low half) and
     scales uint8[rows, ceil(dim/32)], contiguous CUDA tensors.  A read-only
-    copy of a table at 4.25 bits a value; see mx4_quantize."""
+    copy of a table at 4.25 bits a value; see mx4_quantize.  Where dim is no
+    multiple of 32 the codes behind a row are zero (products read them)."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, dim: int):
         _dev(codes, torch.uint8, "codes")
@@ -131,7 +132,7 @@ class MX4:
         return self._lookup(None, self.rows, (self.rows,), 1.0, dtype, None, out, stream)
 
     def _lookup(self, ids, n, shape, scale, dtype, pad, out, stream):
-        with _On(self.device, stream) as st:
+        with _On(self.device, stream, (self.codes, self.scales, ids, out, self._err)) as st:
             if ids is not None and self._err is None:
                 if torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("the first embed of a table makes its error flag: call it before a capture")
@@ -162,7 +163,7 @@ def mx4_quantize(x: torch.Tensor, stream=None) -> MX4:
     rows, dim = x.shape
     _, ld = _rows(x, dim, x.device, "x")
     nb = -(-dim // MX_BLOCK)
-    with _On(x.device, stream) as st:
+    with _On(x.device, stream, (x,)) as st:
         codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=x.device)
         scales = torch.empty((rows, nb), dtype=torch.uint8, device=x.device)
         check(lib().ps_mx4_quantize(rows, dim, _type(x.dtype, "x"), _ptr(x), ld, _ptr(codes), _ptr(scales), st))
@@ -177,7 +178,7 @@ def mx4_product(a: MX4, b: MX4, scale: float = 1.0, dtype: torch.dtype = torch.f
         raise ValueError(f"rows of {a.dim} and of {b.dim} values")
     if a.device != b.device:
         raise TypeError("the operands must be on one device")
-    with _On(a.device, stream) as st:
+    with _On(a.device, stream, (a.codes, a.scales, b.codes, b.scales, out)) as st:
         if out is None:
             out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
         if tuple(out.shape) != (a.rows, b.rows):

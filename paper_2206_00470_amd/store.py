@@ -66,14 +66,20 @@ def _rows(t: torch.Tensor, cols: int, device, name: str):
 class _On:
     """The device of a call's tensors made current, and the stream of the call
     (the device's current one if none is given) the one that new tensors
-    belong to."""
+    belong to.  `used`: tensors of the call that may belong to another stream;
+    their memory is kept until the call's stream is through with it."""
 
     __slots__ = ("device", "inner")
 
-    def __init__(self, device, stream):
+    def __init__(self, device, stream, used=()):
         self.device, self.inner = device, None
         if stream is not None:
+            if stream.device != device:
+                raise ValueError(f"a stream of {stream.device} for tensors on {device}")
             self.inner = torch.cuda.stream(stream)
+            for t in used:
+                if t is not None:
+                    t.record_stream(stream)
         elif torch.cuda.current_device() != device.index:
             self.inner = torch.cuda.device(device)
 
@@ -296,7 +302,7 @@ class Store:
         outside the table gives zeros and raises the sticky error.  out:
         equidistant rows, in place of a new tensor (dtype is then its own)."""
         n = self._ids(ids)
-        with _On(self.W.device, stream) as st:
+        with _On(self.W.device, stream, (ids, out)) as st:
             if out is None:
                 out = torch.empty((*ids.shape, self.dim), dtype=dtype, device=self.W.device)
             rows, ld = _rows(out, self.dim, self.W.device, "out")
@@ -323,7 +329,7 @@ class Store:
         to."""
         if accumulate and out is None:
             raise ValueError("accumulate needs the gradient to add to (out)")
-        with _On(self.W.device, stream) as st:
+        with _On(self.W.device, stream, (ids, dout, out)) as st:
             n, ld, kind, ws = self._grad_args(ids, dout)
             if out is None:
                 out = torch.empty((self.num_keys, self.dim), dtype=dtype, device=self.W.device)
@@ -340,7 +346,7 @@ class Store:
         """The same gradient as merged rows: (uniq, rows), the distinct ids in
         ascending order and their gradient rows, as push takes them.  Waits
         for the number of distinct ids."""
-        with _On(self.W.device, stream) as st:
+        with _On(self.W.device, stream, (ids, dout)) as st:
             n, ld, kind, ws = self._grad_args(ids, dout)
             uniq = torch.empty(n, dtype=torch.int64, device=self.W.device)
             rows = torch.empty((n, self.dim), dtype=dtype, device=self.W.device)

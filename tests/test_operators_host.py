@@ -95,6 +95,16 @@ def test_mx4_refuses_bad_arguments():
     assert p(m=1 << 30, n=1 << 40, ld=1 << 40) == BIG
 
 
+def test_sizes_beyond_a_grid_are_refused():
+    """A launch counts its threads in 32 bits."""
+    L = _lib.lib()
+    assert L.ps_mx4_quantize(1 << 40, 64, F32, P(), 64, P(), P(), None) == BIG
+    assert L.ps_mx4_quantize(1 << 30, 1024, F32, P(), 1024, P(), P(), None) == BIG
+    assert L.ps_mx4_embed(P(), P(), 1 << 41, 64, None, 1 << 40, NOPAD, 1.0, F32, P(), 64, None, None) == BIG
+    assert L.ps_mx4_embed(P(), P(), 100, 4096, P(), 1 << 26, NOPAD, 1.0, F32, P(), 4096, P(), None) == BIG
+    assert L.ps_mx4_product(1 << 22, 1 << 28, 64, P(), P(), P(), P(), 1.0, F32, P(), 1 << 28, None) == BIG
+
+
 def test_binding_refuses_host_tensors():
     with pytest.raises(TypeError):
         ClipPlan([torch.zeros(4)])
