@@ -12,7 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import check, lib
-from .store import _dev, _On, _pad, _ptr, _rows, _type
+from .store import _dev, _On, _pad, _rows, _type
 
 
 # ---------------------------------------------------------------------------- norm and clipping
@@ -58,13 +58,13 @@ class ClipPlan:
     def _buffers(self):
         # of its own per call: a captured call keeps the ones it was captured with
         buf = torch.empty(1 + self._words, dtype=torch.float64, device=self.device)
-        return buf[:1], C.c_void_p(buf.data_ptr() + 8), 8 * self._words
+        return buf[:1], buf.data_ptr() + 8, 8 * self._words
 
     def norm(self, stream=None) -> torch.Tensor:
         """The global norm of the gradients, float64[1]."""
         with _On(self.device, stream, self.grads) as st:
             norm, ws, wsb = self._buffers()
-            check(lib().ps_grad_norm(self._n, self._in, self._numel, self._types, _ptr(norm), ws, wsb, st))
+            check(lib().ps_grad_norm(self._n, self._in, self._numel, self._types, norm.data_ptr(), ws, wsb, st))
         return norm
 
     def clip(self, max_norm: float, stream=None) -> torch.Tensor:
@@ -72,8 +72,8 @@ class ClipPlan:
         larger, to the outputs; returns the norm before, float64[1]."""
         with _On(self.device, stream, (*self.grads, *self.out) if stream is not None else ()) as st:
             norm, ws, wsb = self._buffers()
-            check(lib().ps_clip_grads(self._n, self._in, self._out, self._numel, self._types, max_norm, _ptr(norm), ws,
-                                      wsb, st))
+            check(lib().ps_clip_grads(self._n, self._in, self._out, self._numel, self._types, max_norm,
+                                      norm.data_ptr(), ws, wsb, st))
         return norm
 
 
@@ -137,14 +137,16 @@ class MX4:
                 if torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("the first embed of a table makes its error flag: call it before a capture")
                 self._err = torch.zeros(2, dtype=torch.int32, device=self.device)
+            ld = self.dim
             if out is None:
-                out = torch.empty((*shape, self.dim), dtype=dtype, device=self.device)
-            rows, ld = _rows(out, self.dim, self.device, "out")
-            if rows != n:
-                raise ValueError("out must have one row per id")
-            check(lib().ps_mx4_embed(_ptr(self.codes), _ptr(self.scales), self.rows, self.dim, _ptr(ids), n, _pad(pad),
-                                     scale, _type(out.dtype, "out"), _ptr(out), ld,
-                                     _ptr(self._err if ids is not None else None), st))
+                out = torch.empty((*shape, ld), dtype=dtype, device=self.device)
+            else:
+                rows, ld = _rows(out, ld, self.device, "out")
+                if rows != n:
+                    raise ValueError("out must have one row per id")
+            at, err = (ids.data_ptr(), self._err.data_ptr()) if ids is not None else (None, None)
+            check(lib().ps_mx4_embed(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.dim, at, n, _pad(pad),
+                                     scale, _type(out.dtype, "out"), out.data_ptr(), ld, err, st))
         return out
 
     def error(self) -> int:
@@ -166,7 +168,8 @@ def mx4_quantize(x: torch.Tensor, stream=None) -> MX4:
     with _On(x.device, stream, (x,)) as st:
         codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=x.device)
         scales = torch.empty((rows, nb), dtype=torch.uint8, device=x.device)
-        check(lib().ps_mx4_quantize(rows, dim, _type(x.dtype, "x"), _ptr(x), ld, _ptr(codes), _ptr(scales), st))
+        check(lib().ps_mx4_quantize(rows, dim, _type(x.dtype, "x"), x.data_ptr(), ld, codes.data_ptr(),
+                                    scales.data_ptr(), st))
     return MX4.__new__(MX4)._set(codes, scales, dim)
 
 
@@ -184,6 +187,6 @@ def mx4_product(a: MX4, b: MX4, scale: float = 1.0, dtype: torch.dtype = torch.f
         if tuple(out.shape) != (a.rows, b.rows):
             raise ValueError(f"out must be [{a.rows}, {b.rows}]")
         _, ld = _rows(out, b.rows, a.device, "out")
-        check(lib().ps_mx4_product(a.rows, b.rows, a.dim, _ptr(a.codes), _ptr(a.scales), _ptr(b.codes),
-                                   _ptr(b.scales), scale, _type(out.dtype, "out"), _ptr(out), ld, st))
+        check(lib().ps_mx4_product(a.rows, b.rows, a.dim, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
+                                   b.scales.data_ptr(), scale, _type(out.dtype, "out"), out.data_ptr(), ld, st))
     return out

@@ -303,12 +303,15 @@ class Store:
         equidistant rows, in place of a new tensor (dtype is then its own)."""
         n = self._ids(ids)
         with _On(self.W.device, stream, (ids, out)) as st:
+            ld = self.dim
             if out is None:
-                out = torch.empty((*ids.shape, self.dim), dtype=dtype, device=self.W.device)
-            rows, ld = _rows(out, self.dim, self.W.device, "out")
-            if rows != n:
-                raise ValueError("out must have one row per id")
-            check(lib().ps_embed(self._h, _ptr(ids), n, _pad(pad), scale, _type(out.dtype, "out"), _ptr(out), ld, st))
+                out = torch.empty((*ids.shape, ld), dtype=dtype, device=self.W.device)
+            else:
+                rows, ld = _rows(out, ld, self.W.device, "out")
+                if rows != n:
+                    raise ValueError("out must have one row per id")
+            check(lib().ps_embed(self._h, ids.data_ptr(), n, _pad(pad), scale, _type(out.dtype, "out"), out.data_ptr(), ld,
+                                 st))
         return out
 
     def _grad_args(self, ids, dout):
@@ -331,14 +334,16 @@ class Store:
             raise ValueError("accumulate needs the gradient to add to (out)")
         with _On(self.W.device, stream, (ids, dout, out)) as st:
             n, ld, kind, ws = self._grad_args(ids, dout)
+            out_ld = self.dim
             if out is None:
                 out = torch.empty((self.num_keys, self.dim), dtype=dtype, device=self.W.device)
-            rows, out_ld = _rows(out, self.dim, self.W.device, "out")
-            if rows != self.num_keys:
-                raise ValueError("out must have one row per key")
-            check(lib().ps_embed_grad(self._h, _ptr(ids), n, _pad(pad), scale, kind, _ptr(dout), ld,
-                                      _type(out.dtype, "out"), _ptr(out), out_ld, int(accumulate), _ptr(ws), ws.numel(),
-                                      st))
+            else:
+                rows, out_ld = _rows(out, self.dim, self.W.device, "out")
+                if rows != self.num_keys:
+                    raise ValueError("out must have one row per key")
+            check(lib().ps_embed_grad(self._h, ids.data_ptr(), n, _pad(pad), scale, kind, dout.data_ptr(), ld,
+                                      _type(out.dtype, "out"), out.data_ptr(), out_ld, int(accumulate), ws.data_ptr(),
+                                      ws.numel(), st))
         return out
 
     def embed_grad_rows(self, ids: torch.Tensor, dout: torch.Tensor, scale: float = 1.0, pad: int | None = None,
@@ -353,9 +358,9 @@ class Store:
             # the number comes straight to host memory: no copy to wait for behind the kernels
             count = torch.empty(1, dtype=torch.int32, pin_memory=True)
             # (rows: an address even where there are no ids)
-            check(lib().ps_embed_grad_rows(self._h, _ptr(ids), n, _pad(pad), scale, kind, _ptr(dout), ld,
-                                           _type(dtype, "dtype"), _ptr(uniq), _ptr(rows if n else count), self.dim,
-                                           _ptr(count), _ptr(ws), ws.numel(), st))
+            check(lib().ps_embed_grad_rows(self._h, ids.data_ptr(), n, _pad(pad), scale, kind, dout.data_ptr(), ld,
+                                           _type(dtype, "dtype"), uniq.data_ptr(), (rows if n else count).data_ptr(),
+                                           self.dim, count.data_ptr(), ws.data_ptr(), ws.numel(), st))
             torch.cuda.current_stream(self.W.device).synchronize()
             U = int(count)
         return uniq[:U], rows[:U]
