@@ -76,20 +76,18 @@ namespace {
 // Blocks folded together: a run over x blocks is finished from about x / f + 2 f
 // partial rows, sixteen of them at a time, and the commonest token has a tenth
 // or so of a batch.  Up to 256 blocks none are, which saves a launch.
-int fold_blocks(int64_t blocks) {
-  return blocks <= 256 ? 1024 : blocks < 16384 ? 16 : blocks < (1 << 20) ? 64 : 256;
-}
+int log_fold(int64_t blocks) { return blocks <= 256 ? 10 : blocks < 16384 ? 4 : blocks < (1 << 20) ? 6 : 8; }
 
 // Positions of a block: fewer rows are added one after another where there are
 // not enough blocks of 16 to fill the units, which costs more partial rows.
 // Measured, with 8 and with 16: 1,021 ids of 300 floats 27.0 and 31.8 us, 8,192
 // of 768 bf16 values 51.3 and 58.1; 20,000 of 2,048 65.8 and 64.0, 300,000 of 64
 // 114 and 105, 1M of 100 floats 317 and 302.
-int block_of(int64_t n, int dim) { return n * int64_t(dim) < (int64_t(1) << 24) ? 8 : 16; }
+int log_block(int64_t n, int dim) { return n * int64_t(dim) < (int64_t(1) << 24) ? 3 : 4; }
 
 struct GradPlan {
   size_t order = 0;        // the sort's share, at the start
-  int block = 0;           // positions of a block
+  int log_block = 0;       // positions of a block, as a power of two
   double* partial = nullptr;
   double* fold = nullptr;
   int4* split_list = nullptr;
@@ -109,10 +107,10 @@ GradPlan plan_grad(void* ws, int64_t n, int dim) {
     off += bytes;
     return q;
   };
-  p.block = block_of(n, dim);
-  const int64_t blocks = div_up(n, p.block);
+  p.log_block = log_block(n, dim);
+  const int64_t blocks = div_up(n, int64_t(1) << p.log_block);
   p.partial = reinterpret_cast<double*>(take(size_t(2) * blocks * dim * sizeof(double)));
-  p.fold = reinterpret_cast<double*>(take(size_t(blocks / fold_blocks(blocks)) * dim * sizeof(double)));
+  p.fold = reinterpret_cast<double*>(take(size_t(blocks >> log_fold(blocks)) * dim * sizeof(double)));
   p.split_list = reinterpret_cast<int4*>(take(size_t(blocks) * sizeof(int4)));
   p.split_count = reinterpret_cast<uint32_t*>(take(sizeof(uint32_t)));
   p.tile_heads = reinterpret_cast<uint32_t*>(take(size_t(div_up(n, RUNS_TILE)) * sizeof(uint32_t)));
@@ -187,7 +185,7 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
   int log_lanes = 2;
   while ((1 << log_lanes) < WAVE && (1 << log_lanes) < vectors) ++log_lanes;
   const int slices = (int)div_up(vectors, 1 << log_lanes);
-  const int64_t blocks = div_up(c.n, p.block);
+  const int64_t blocks = div_up(c.n, int64_t(1) << p.log_block);
   const int64_t grid = div_up(blocks, BLOCK >> log_lanes);
   if (grid > GRID_MAX || div_up(c.n, BLOCK) > GRID_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld ids of %d exceed the merge's grid", (long long)c.n, t.dim);
 
@@ -210,16 +208,16 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
       RAISE_HIP(hipGetLastError());
     }
     hipLaunchKernelGGL(k_runs_write, dim3(tiles), dim3(BLOCK), 0, st, o.keys, c.n, (uint32_t)t.num_keys, p.tile_heads,
-                       (int)scan, p.block, c.uniq, o.seg_off, p.block_run, c.num_unique);
+                       (int)scan, p.log_block, c.uniq, o.seg_off, p.block_run, c.num_unique);
     RAISE_HIP(hipGetLastError());
   }
   const GradRuns g{o.keys, o.perm, c.n, (uint32_t)t.num_keys, rows ? o.seg_off : nullptr, o.hdr,
-                   own_runs ? p.block_run : nullptr, c.num_unique, p.partial, p.block, fold_blocks(blocks),
+                   own_runs ? p.block_run : nullptr, c.num_unique, p.partial, p.log_block, log_fold(blocks),
                    p.split_list, p.split_count};
   const ps_status r = with_type(c.in_type, [&]<class IT>(IT) -> ps_status {
     return with_width(vw, [&]<int VW>() -> ps_status {
       if constexpr (sizeof(IT) * VW <= 16) {
-        auto kernel = p.block == 8 ? k_grad_merge<IT, VW, 8> : k_grad_merge<IT, VW, 16>;
+        auto kernel = p.log_block == 3 ? k_grad_merge<IT, VW, 8> : k_grad_merge<IT, VW, 16>;
         hipLaunchKernelGGL(kernel, dim3(grid, slices), dim3(BLOCK), (BLOCK >> log_lanes) * sizeof(GradMeta), st, g,
                            static_cast<const IT*>(c.dout), c.in_ld, t.dim, log_lanes, c.scale, c.out);
         RAISE_HIP(hipGetLastError());
@@ -230,14 +228,14 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
   if (r) return r;
   if (blocks < 3) return PS_OK;   // no run is longer than its block and the next
   const int col_slices = (int)div_up(t.dim, WAVE);
-  const int64_t supers = blocks / fold_blocks(blocks);
+  const int64_t supers = blocks >> log_fold(blocks);
   if (supers > 1) {   // (the first is never folded)
-    hipLaunchKernelGGL(k_grad_fold, dim3(std::min<int64_t>(div_up(supers * col_slices, WAVES_PER_BLOCK), 2048)),
-                       dim3(BLOCK), 0, st, g, supers, t.dim, col_slices, p.fold);
+    hipLaunchKernelGGL(k_grad_fold, dim3(std::min<int64_t>(supers * col_slices, 2048)), dim3(BLOCK), 0, st, g, (int)supers,
+                       t.dim, col_slices, p.fold);
     RAISE_HIP(hipGetLastError());
   }
-  hipLaunchKernelGGL(k_grad_finish, dim3(std::min<int64_t>(div_up(blocks * col_slices, WAVES_PER_BLOCK), 2048)), dim3(BLOCK), 0, st, g, t.dim,
-                     col_slices, p.fold, c.scale, c.out);
+  hipLaunchKernelGGL(k_grad_finish, dim3(std::min<int64_t>(blocks * col_slices, 2048)), dim3(BLOCK), 0, st, g, t.dim, col_slices,
+                     p.fold, c.scale, c.out);
   RAISE_HIP(hipGetLastError());
   return PS_OK;
 }

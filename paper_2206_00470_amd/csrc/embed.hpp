@@ -71,7 +71,7 @@ __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64
 // whole.  A longer run leaves one fp64 partial row per block: in the even slot
 // of the block where it comes in from the block before or starts with the
 // block, in the odd slot where it starts inside.  k_grad_fold adds the even
-// slots of `fold` blocks that one run fills, k_grad_finish adds the rest.
+// slots of as many blocks (a power of two) as one run fills, k_grad_finish adds the rest.
 constexpr int GRAD_BLOCK_MAX = 16;   // positions of a block: 16, or 8 in small calls
 
 // Where a token's gradient row goes: row `key` of the dense form, or the
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(BLOCK) void k_runs_scan(uint32_t* __restrict__ tile
 }
 
 __global__ __launch_bounds__(BLOCK) void k_runs_write(const uint32_t* __restrict__ keys, int64_t n, uint32_t sentinel,
-                                                      const uint32_t* __restrict__ tile_heads, int scanned, int block,
+                                                      const uint32_t* __restrict__ tile_heads, int scanned, int log_block,
                                                       int64_t* __restrict__ uniq, int32_t* __restrict__ seg_off,
                                                       int32_t* __restrict__ block_run,
                                                       int32_t* __restrict__ num_unique) {
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(BLOCK) void k_runs_write(const uint32_t* __restrict
 #pragma unroll
   for (int i = 0; i < RUNS_ITEMS; ++i) {
     const bool head = (heads >> i) & 1u;
-    if ((p + i) % block == 0 && p + i < n) block_run[(p + i) / block] = (int32_t)(u + head) - 1;
+    if (((p + i) & ((1 << log_block) - 1)) == 0 && p + i < n) block_run[(p + i) >> log_block] = (int32_t)(u + head) - 1;
     if (head) {
       uniq[u] = (int64_t)k[i];
       seg_off[u] = (int32_t)(p + i);
@@ -223,8 +223,8 @@ struct GradRuns {
   const int32_t* block_run;  // or, from k_runs_write, the run of each block's first position
   int32_t* num_unique;     // rows form: receives the number of rows
   double* partial;         // [2 * blocks][dim]
-  int block;               // positions of a block
-  int fold;                // blocks folded together
+  int log_block;           // positions of a block, and blocks folded together, as powers of two
+  int log_fold;
   int4* split_list;        // the longer runs: first position, key, index of the run
   uint32_t* split_count;
 };
@@ -341,93 +341,101 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
   }
 }
 
-// Adds rows row(k), k = 0 .. count-1, of fp64 column col in their order, FU of
-// them in flight.
+// Adds rows row(k), k = 0 .. count-1, of fp64 column col: wave w of the
+// workgroup the rows w, w + 4, ... in their order, SUM_FLIGHT of them in flight,
+// then the waves' sums in wave order.  The time of a long run is that of a chain
+// of loads, hence a workgroup for each (a wave each, and all waves on one run of
+// few rows only where it is long: 400,000 ids of 16 floats over 1,000 rows 83
+// and 71 us against 69, 300,000 of 64 over 50,000 96 and 88 against 84,
+// 20,000 of 2,048 over 500, many runs of few rows, 55 and 59 against 55).
+constexpr int SUM_FLIGHT = 8;
+
 template <class RowAt>
-__device__ __forceinline__ double sum_rows(RowAt row, int64_t count, bool active, int col) {
-  constexpr int FU = 16;
+__device__ __forceinline__ double sum_rows(RowAt row, int count, bool active, int col, double* smem) {
+  const int w = threadIdx.x / WAVE;
   double acc = 0.0;
-  int64_t k = 0;
-  for (; k + FU <= count; k += FU) {
-    double x[FU];
+  for (int k = w; k < count; k += SUM_FLIGHT * WAVES_PER_BLOCK) {
+    double x[SUM_FLIGHT];
 #pragma unroll
-    for (int f = 0; f < FU; ++f) x[f] = active ? row(k + f)[col] : 0.0;
+    for (int f = 0; f < SUM_FLIGHT; ++f)
+      x[f] = active && k + f * WAVES_PER_BLOCK < count ? row(k + f * WAVES_PER_BLOCK)[col] : 0.0;
 #pragma unroll
-    for (int f = 0; f < FU; ++f) acc += x[f];
+    for (int f = 0; f < SUM_FLIGHT; ++f) acc += k + f * WAVES_PER_BLOCK < count ? x[f] : 0.0;
   }
-  if (k < count) {
-    double x[FU];
+  smem[threadIdx.x] = acc;
+  __syncthreads();
+  double t = 0.0;
 #pragma unroll
-    for (int f = 0; f < FU; ++f) x[f] = active && k + f < count ? row(k + f)[col] : 0.0;
-#pragma unroll
-    for (int f = 0; f < FU; ++f)
-      if (k + f < count) acc += x[f];
-  }
-  return acc;
+  for (int i = 0; i < WAVES_PER_BLOCK; ++i) t += smem[i * WAVE + lane_id()];
+  __syncthreads();
+  return t;
 }
 
-// fold[s] = the even slots of blocks [s * g.fold, (s + 1) * g.fold)
+// fold[s] = the even slots of blocks [s << g.log_fold, (s + 1) << g.log_fold)
 // where one run comes into the first of them and into the last (so into all).
-// One wave per column slice, here and below.
-__global__ __launch_bounds__(BLOCK) void k_grad_fold(GradRuns g, int64_t supers, int dim, int slices,
+// One workgroup per 64 columns, here and below.
+__global__ __launch_bounds__(BLOCK) void k_grad_fold(GradRuns g, int supers, int dim, int slices,
                                                      double* __restrict__ fold) {
-  const int64_t step = (int64_t)gridDim.x * WAVES_PER_BLOCK;
-  for (int64_t e = (int64_t)blockIdx.x * WAVES_PER_BLOCK + threadIdx.x / WAVE; e < supers * slices; e += step) {
-    const int64_t s = e / slices;
-    const int col = (int)(e - s * slices) * WAVE + lane_id();
-    const int64_t b0 = s * g.fold;
+  __shared__ double smem[BLOCK];
+  for (uint32_t e = blockIdx.x; e < (uint32_t)supers * (uint32_t)slices; e += gridDim.x) {
+    const uint32_t s = e / (uint32_t)slices;
+    const int col = (int)(e - s * (uint32_t)slices) * WAVE + lane_id();
+    const int64_t b0 = (int64_t)s << g.log_fold;
     if (b0 == 0) continue;
-    const uint32_t key = g.keys[b0 * g.block];
-    if (key >= g.sentinel || g.keys[b0 * g.block - 1] != key ||
-        g.keys[(b0 + g.fold - 1) * g.block] != key)
+    const uint32_t key = g.keys[b0 << g.log_block];
+    if (key >= g.sentinel || g.keys[(b0 << g.log_block) - 1] != key ||
+        g.keys[(b0 + (1 << g.log_fold) - 1) << g.log_block] != key)
       continue;
-    const double t = sum_rows([&](int64_t k) { return g.partial + 2 * (b0 + k) * dim; }, g.fold, col < dim, col);
-    if (col < dim) fold[s * dim + col] = t;
+    const double t =
+        sum_rows([&](int k) { return g.partial + 2 * (b0 + k) * dim; }, 1 << g.log_fold, col < dim, col, smem);
+    if (threadIdx.x < WAVE && col < dim) fold[(int64_t)s * dim + col] = t;
   }
 }
 
 // The last block that the run of `key`, which comes into block f, comes into,
 // by the wave's lanes together as in run_at.
-__device__ __forceinline__ int64_t last_block(const GradRuns& g, uint32_t key, int64_t f) {
-  const int64_t blocks = (g.n + g.block - 1) / g.block;
-  int64_t lo = f, len = blocks - f;   // it comes into lo, not into lo + len
+__device__ __forceinline__ int32_t last_block(const GradRuns& g, uint32_t key, int32_t f) {
+  const int32_t blocks = (int32_t)((g.n + (1 << g.log_block) - 1) >> g.log_block);
+  int32_t lo = f, len = blocks - f;   // it comes into lo, not into lo + len
   while (len > 1) {
-    const int64_t step = (len + WAVE - 1) / WAVE;
-    const int64_t at = (lane_id() + 1) * step;
-    const int k = __popcll(__ballot(at < len && g.keys[(lo + at) * g.block] == key));
+    const int32_t step = (len + WAVE - 1) / WAVE;
+    const int32_t at = (lane_id() + 1) * step;
+    const int k = __popcll(__ballot(at < len && g.keys[(int64_t)(lo + at) << g.log_block] == key));
     lo += k * step;
     len = len - k * step < step ? len - k * step : step;
   }
   return lo;
 }
 
-// The runs over several blocks: partial of the first block, of the blocks up
-// to the first folded ones, the folds, and the blocks after them, added in
-// this order.
+// The runs over three blocks and more: partial of the first block, of the
+// blocks up to the first folded ones, the folds, and the blocks after them.
 __global__ __launch_bounds__(BLOCK) void k_grad_finish(GradRuns g, int dim, int slices,
                                                        const double* __restrict__ fold, float scale, GradOut out) {
+  __shared__ double smem[BLOCK];
   const int64_t items = (int64_t)*g.split_count * slices;
-  const int64_t step = (int64_t)gridDim.x * WAVES_PER_BLOCK;
-  for (int64_t e = (int64_t)blockIdx.x * WAVES_PER_BLOCK + threadIdx.x / WAVE; e < items; e += step) {
-    const int64_t r = e / slices;
+  for (int64_t e = blockIdx.x; e < items; e += gridDim.x) {
+    const int64_t r = items <= UINT32_MAX ? (int64_t)((uint32_t)e / (uint32_t)slices) : e / slices;
     const int col = (int)(e - r * slices) * WAVE + lane_id();
     const int4 run = g.split_list[r];
-    const int64_t s0 = run.x;
+    const int32_t s0 = run.x;
     const uint32_t key = (uint32_t)run.y;
-    const int64_t f = s0 / g.block + 1;   // the blocks it comes into: f to l
-    const int64_t l = g.seg_off ? (g.seg_off[run.z + 1] - 1) / g.block : last_block(g, key, f);
-    const int64_t sa = (f + g.fold - 1) / g.fold, sb = (l + 1) / g.fold;
-    const int64_t nf = sb > sa ? sb - sa : 0;
-    const int64_t n1 = nf ? sa * g.fold - f : l - f + 1;
-    const int64_t n3 = nf ? l - sb * g.fold + 1 : 0;
-    auto row = [&](int64_t k) -> const double* {
-      if (k == 0) return g.partial + (2 * (s0 / g.block) + (s0 % g.block != 0 ? 1 : 0)) * dim;
-      if (k <= n1) return g.partial + 2 * (f + k - 1) * dim;
-      if (k <= n1 + nf) return fold + (sa + k - 1 - n1) * dim;
-      return g.partial + 2 * (sb * g.fold + k - 1 - n1 - nf) * dim;
+    const int32_t b0 = s0 >> g.log_block, f = b0 + 1;   // the blocks it comes into: f to l
+    const int32_t l = g.seg_off ? (g.seg_off[run.z + 1] - 1) >> g.log_block : last_block(g, key, f);
+    const int32_t sa = (f + (1 << g.log_fold) - 1) >> g.log_fold, sb = (l + 1) >> g.log_fold;   // folds [sa, sb)
+    const int32_t nf = sb > sa ? sb - sa : 0;
+    const int32_t n1 = nf ? (sa << g.log_fold) - f : l - f + 1;
+    const int32_t n3 = nf ? l - (sb << g.log_fold) + 1 : 0;
+    auto row = [&](int32_t k) -> const double* {
+      int64_t slot;
+      if (k == 0) slot = 2 * (int64_t)b0 + ((s0 & ((1 << g.log_block) - 1)) != 0 ? 1 : 0);
+      else if (k <= n1) slot = 2 * (int64_t)(f + k - 1);
+      else if (k <= n1 + nf) return fold + (int64_t)(sa + k - 1 - n1) * dim;
+      else slot = 2 * (int64_t)((sb << g.log_fold) + k - 1 - n1 - nf);
+      return g.partial + slot * dim;
     };
-    const double t = sum_rows(row, 1 + n1 + nf + n3, col < dim, col);
-    if (col < dim) write_grad_any<1>(out, g.seg_off ? (int64_t)run.z : (int64_t)key, col, &t, scale);
+    const double t = sum_rows(row, 1 + n1 + nf + n3, col < dim, col, smem);
+    if (threadIdx.x < WAVE && col < dim)
+      write_grad_any<1>(out, g.seg_off ? (int64_t)run.z : (int64_t)key, col, &t, scale);
   }
 }
 
