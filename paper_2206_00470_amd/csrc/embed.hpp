@@ -20,7 +20,7 @@ __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64
                                                  int dim, float scale, OT* __restrict__ out, int64_t out_ld) {
   constexpr int U = EMBED_FLIGHT;
   const int64_t q0 = (int64_t)blockIdx.x * (BLOCK * U);
-  const int64_t row0 = q0 / nv.d;
+  const int64_t row0 = row_of(q0, nv.d);
   const uint32_t first = (uint32_t)(q0 - row0 * nv.d) + threadIdx.x;
   int bad = 0, miss = 0;
   int64_t src[U], dst[U];

@@ -19,6 +19,12 @@ constexpr int MX4_FLIGHT = 4;
 // and 33.1, 95.4 and 87.4; 240 MB (301 floats) 96.8 and 57.5, 178 and 164.
 constexpr int64_t LOOKUP_STREAMS = int64_t(80) << 20;
 
+// The row of vector q, d vectors a row (a 64-bit division takes several times as
+// long as one of 32 bits).
+__device__ __forceinline__ int64_t row_of(int64_t q, uint32_t d) {
+  return q <= UINT32_MAX ? (int64_t)((uint32_t)q / d) : q / d;
+}
+
 struct LookupIds {
   const int64_t* ids;   // NULL: row i of the table
   int64_t n;

@@ -108,7 +108,7 @@ ps_status ps_mx4_product(int64_t m, int64_t n, int32_t dim, const uint8_t* a_cod
       if (tq > (GRID_MAX - NUM_XCD) / tt) return raise(PS_ERR_UNSUPPORTED, "%lld x %lld exceed the grid", (long long)m, (long long)n);
       hipLaunchKernelGGL(kernel, dim3(div_up(tq * tt, NUM_XCD) * NUM_XCD), dim3(BLOCK), 0,
                          static_cast<hipStream_t>(stream), A, B, blocks_of(dim),
-                         scale, static_cast<OT*>(out), out_stride, tq);
+                         scale, static_cast<OT*>(out), out_stride, (uint32_t)tq, (uint32_t)tt);
       RAISE_HIP(hipGetLastError());
       return PS_OK;
     };

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_quantize(const T* __restrict__ x,
                                                         SmallDiv per_row, uint32_t* __restrict__ codes,
                                                         uint8_t* __restrict__ scales) {
   const int64_t q0 = (int64_t)blockIdx.x * BLOCK;
-  const int64_t row0 = q0 / per_row.d;
+  const int64_t row0 = row_of(q0, per_row.d);
   const uint32_t a = (uint32_t)(q0 - row0 * per_row.d) + threadIdx.x;
   const uint32_t dr = quotient(a, per_row);
   const int c = (int)(a - dr * per_row.d) * 8;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__
                                                      int64_t out_ld) {
   constexpr int U = MX4_FLIGHT;
   const int64_t q0 = (int64_t)blockIdx.x * (BLOCK * U);
-  const int64_t row0 = q0 / nv.d;
+  const int64_t row0 = row_of(q0, nv.d);
   const uint32_t first = (uint32_t)(q0 - row0 * nv.d) + threadIdx.x;
   int bad = 0, miss = 0;
   constexpr int VW = 16 / sizeof(OT);
@@ -244,20 +244,21 @@ __device__ __forceinline__ mx_operand mx_words(const words4& c) {
 // lie side by side (tiles under each other, 2^k bytes apart, meet in few
 // channels of the memory).  Measured, 2,048 x 131,072 of dim 64 and 512, bf16:
 // tiles under each other 134 and 160 us, groups 99 and 157.
-constexpr int MX_GROUP = 16;
+constexpr uint32_t MX_GROUP = 16;
 
-__device__ __forceinline__ void mx_tile(int64_t tiles_q, int64_t tiles_b, int64_t& tb, int64_t& tq) {
+// (tiles are counted in 32 bits, as workgroups are)
+__device__ __forceinline__ void mx_tile(uint32_t tiles_q, uint32_t tiles_b, uint32_t& tb, uint32_t& tq) {
   if (tiles_q == 1) {
     tb = blockIdx.x;
     tq = 0;
     return;
   }
-  const int64_t tile = (int64_t)(blockIdx.x % NUM_XCD) * (gridDim.x / NUM_XCD) + blockIdx.x / NUM_XCD;
-  const int64_t group = tile / (MX_GROUP * tiles_q), rest = tile - group * (MX_GROUP * tiles_q);
-  const int64_t left = tiles_b - group * MX_GROUP;
-  const int64_t wide = left < 1 ? 1 : left < MX_GROUP ? left : MX_GROUP;
+  const uint32_t tile = (blockIdx.x % NUM_XCD) * (gridDim.x / NUM_XCD) + blockIdx.x / NUM_XCD;
+  const uint32_t group = tile / (MX_GROUP * tiles_q), rest = tile - group * (MX_GROUP * tiles_q);
+  const uint32_t before = group * MX_GROUP;
+  const uint32_t wide = before >= tiles_b ? 1 : tiles_b - before < MX_GROUP ? tiles_b - before : MX_GROUP;
   tq = rest / wide;
-  tb = group * MX_GROUP + (rest - tq * wide);
+  tb = before + (rest - tq * wide);
   if (tq >= tiles_q) tb = tiles_b;   // beyond the last tile
 }
 
@@ -265,7 +266,8 @@ __device__ __forceinline__ void mx_tile(int64_t tiles_q, int64_t tiles_b, int64_
 // stand WQ x WT.  Rows of C are stored 16 bytes at a time wherever they start.
 template <class OT, int QT, int TT, int WQ, int WT, bool NT>
 __global__ __launch_bounds__(BLOCK, 4) void k_mx4_product(MxRows A, MxRows B, int blocks_row, float scale,
-                                                       OT* __restrict__ C, int64_t ldc, int64_t tiles_q) {
+                                                       OT* __restrict__ C, int64_t ldc, uint32_t tiles_q,
+                                                       uint32_t tiles_b) {
   constexpr int VW = 16 / sizeof(OT);
   constexpr int ET = sizeof(OT) == 2 && TT % 4 == 0 ? 4 : 2;   // tiles that leave together: rows of 256 or 128 bytes
   static_assert(WQ * WT == WAVES_PER_BLOCK && TT % ET == 0, "four waves, whole rows");
@@ -274,14 +276,15 @@ __global__ __launch_bounds__(BLOCK, 4) void k_mx4_product(MxRows A, MxRows B, in
   constexpr size_t kStage = (RA + RB) * 8 * sizeof(words4), kOut = WAVES_PER_BLOCK * 32 * PITCH * sizeof(OT);
   __shared__ words4 lds[(kStage > kOut ? kStage : kOut) / sizeof(words4)];
   const int w = threadIdx.x / WAVE, l = lane_id();
-  int64_t tb, tq;
-  mx_tile(tiles_q, (B.rows + RB - 1) / RB, tb, tq);
-  if (tb * RB >= B.rows) return;   // (the grid is a multiple of the dies)
+  uint32_t tb, tq;
+  mx_tile(tiles_q, tiles_b, tb, tq);
+  if (tb >= tiles_b) return;   // (the grid is a multiple of the dies)
   const int wa = w / WT * QT * 32, wb = w % WT * TT * 32;   // the wave's rows in the tile
-  const int64_t i0 = tq * RA + wa, j0 = tb * RB + wb;
+  const int64_t i0 = (int64_t)tq * RA + wa, j0 = (int64_t)tb * RB + wb;
   const int half = l / 32, r = l % 32;
   words4 *sa = lds, *sb = lds + RA * 8;
-  const MxTile ta = mx_rows(A, tq * RA, RA, blocks_row), tbl = mx_rows(B, tb * RB, RB, blocks_row);
+  const MxTile ta = mx_rows(A, (int64_t)tq * RA, RA, blocks_row),
+               tbl = mx_rows(B, (int64_t)tb * RB, RB, blocks_row);
   mx_acc acc[QT][TT];
 #pragma unroll
   for (int q = 0; q < QT; ++q)
