@@ -216,21 +216,31 @@ __device__ __forceinline__ void mx_stage(const MxTile& t, int k0, int blocks_row
   }
 }
 
-// The scale bytes of blocks kb .. kb+count-1 of a row (count at most 4), 1
-// where they are beyond its end.
-template <bool FULL>
-__device__ __forceinline__ uint32_t mx_scales(const MxTile& t, int row, int kb, int count, int blocks_row) {
-  const uint8_t* p = t.scales + (uint32_t)((row < t.last ? row : t.last) * blocks_row + kb);
-  uint32_t s;
-  if constexpr (FULL) {
-    __builtin_memcpy(&s, p, 4);
-  } else {
-    s = 0x7f7f7f7fu;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (q < count && kb + q < blocks_row) s ^= (uint32_t)(p[q] ^ 0x7fu) << (8 * q);
+// SW words of a row's scale bytes from block k0 on, 1 where they are beyond its end.
+template <int SW>
+__device__ __forceinline__ void mx_scales(const MxTile& t, int row, int k0, int blocks_row, uint32_t (&s)[SW]) {
+  const uint8_t* p = t.scales + (uint32_t)((row < t.last ? row : t.last) * blocks_row + k0);
+  const int left = blocks_row - k0;
+  if (left >= 4 * SW) {
+    __builtin_memcpy(s, p, 4 * SW);
+    return;
   }
-  return s;
+#pragma unroll
+  for (int i = 0; i < SW; ++i) {
+    const int have = left - 4 * i;   // of the word's bytes, where below 4
+    s[i] = 0x7f7f7f7fu;
+    if (have >= 4) {
+      __builtin_memcpy(&s[i], p + 4 * i, 4);
+    } else if (have > 0 && blocks_row >= 4) {   // the row's last four, those before the word's shifted out
+      uint32_t x;
+      __builtin_memcpy(&x, p + left - 4, 4);
+      s[i] = (uint32_t)((0x7f7f7f7full << 32 | x) >> (32 - 8 * have));
+    } else if (have > 0) {
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        if (q < have) s[i] ^= (uint32_t)(p[4 * i + q] ^ 0x7fu) << (8 * q);
+    }
+  }
 }
 
 __device__ __forceinline__ mx_operand mx_words(const words4& c) {
@@ -275,6 +285,8 @@ __global__ __launch_bounds__(BLOCK, 4) void k_mx4_product(MxRows A, MxRows B, in
   constexpr int RA = WQ * QT * 32, RB = WT * TT * 32;   // rows of the workgroup's tile
   constexpr size_t kStage = (RA + RB) * 8 * sizeof(words4), kOut = WAVES_PER_BLOCK * 32 * PITCH * sizeof(OT);
   __shared__ words4 lds[(kStage > kOut ? kStage : kOut) / sizeof(words4)];
+  constexpr int SW = 2;   // words of scales staged together
+  __shared__ uint32_t scales[SW][RA + RB];
   const int w = threadIdx.x / WAVE, l = lane_id();
   uint32_t tb, tq;
   mx_tile(tiles_q, tiles_b, tb, tq);
@@ -311,23 +323,38 @@ __global__ __launch_bounds__(BLOCK, 4) void k_mx4_product(MxRows A, MxRows B, in
         acc[q][t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[t], fa[q], acc[q][t], 4, 4, K, (int)xb[t], K,
                                                                     (int)xa[q]);
   };
+  constexpr int SR = (RA + RB + BLOCK - 1) / BLOCK;   // rows whose scales a thread brings
+  uint32_t sc[SR][SW];
   auto stage = [&](int k0) {
     if (k0 > 0) __syncthreads();
     mx_stage<RB>(tbl, k0, blocks_row, sb);
     mx_stage<RA>(ta, k0, blocks_row, sa);
-  };
-  auto staged = [&] {
+    if (k0 % (4 * SW) == 0) {
+#pragma unroll
+      for (int i = 0; i < SR; ++i) {
+        const int row = i * BLOCK + threadIdx.x;
+        if (row < RA) mx_scales(ta, row, k0, blocks_row, sc[i]);
+        else if (row < RA + RB) mx_scales(tbl, row - RA, k0, blocks_row, sc[i]);
+      }
+    }
+    if (k0 % (4 * SW) == 0) {
+#pragma unroll
+      for (int i = 0; i < SR; ++i)
+#pragma unroll
+        for (int q = 0; q < SW; ++q)
+          if (i * BLOCK + (int)threadIdx.x < RA + RB) scales[q][i * BLOCK + threadIdx.x] = sc[i][q];
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
   int k0 = 0;
   for (; k0 + 8 <= blocks_row; k0 += 8) {
     stage(k0);
+    const uint32_t* s = scales[k0 % (4 * SW) / 4 + half];
 #pragma unroll
-    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<true>(tbl, wb + t * 32 + r, k0 + 4 * half, 4, blocks_row);
+    for (int t = 0; t < TT; ++t) xb[t] = s[RA + wb + t * 32 + r];
 #pragma unroll
-    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<true>(ta, wa + q * 32 + r, k0 + 4 * half, 4, blocks_row);
-    staged();
+    for (int q = 0; q < QT; ++q) xa[q] = s[wa + q * 32 + r];
     multiply.template operator()<0, true>(4 * half, 8);
     multiply.template operator()<1, true>(4 * half, 8);
     multiply.template operator()<2, true>(4 * half, 8);
@@ -336,11 +363,15 @@ __global__ __launch_bounds__(BLOCK, 4) void k_mx4_product(MxRows A, MxRows B, in
   if (k0 < blocks_row) {   // up to seven blocks, halved between the lanes below 32 and above
     const int rem = blocks_row - k0, per = (rem + 1) / 2;
     stage(k0);
+    const int w0 = k0 % (4 * SW) / 4;
+    // four bytes from byte 0 or `per` (at most 4) of the eight
+    auto scale_word = [&](int row) {
+      return (uint32_t)(((uint64_t)scales[w0 + 1][row] << 32 | scales[w0][row]) >> (8 * per * half));
+    };
 #pragma unroll
-    for (int t = 0; t < TT; ++t) xb[t] = mx_scales<false>(tbl, wb + t * 32 + r, k0 + per * half, per, blocks_row);
+    for (int t = 0; t < TT; ++t) xb[t] = scale_word(RA + wb + t * 32 + r);
 #pragma unroll
-    for (int q = 0; q < QT; ++q) xa[q] = mx_scales<false>(ta, wa + q * 32 + r, k0 + per * half, per, blocks_row);
-    staged();
+    for (int q = 0; q < QT; ++q) xa[q] = scale_word(wa + q * 32 + r);
     multiply.template operator()<0, false>(per * half, rem);
     if (per > 1) multiply.template operator()<1, false>(per * half, rem);
     if (per > 2) multiply.template operator()<2, false>(per * half, rem);
