@@ -170,10 +170,10 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* o, int64_t count, Coe
 
 // The chunks go from the last to the first: the ones read last for the norm are
 // still in the last-level cache.  NT (large outputs that are not their inputs)
-// writes past the caches.  Measured, 500M bf16 values in 291 tensors: 582 us in
-// the norm's order, 575 backwards, 536 past the caches (178 of it the norm, 5.6
-// TB/s read; 5.6 TB/s read and written by the rest), 200M fp32 in 400 491, 484
-// and 444; in place 602 and 590 with and without.
+// writes past the caches.  Measured, 500M bf16 values in 291 tensors: 567 us
+// through the caches, 528 past them (174 of it the norm, 5.7 TB/s read; 5.6 TB/s
+// read and written by the rest), 536 in the norm's order; 200M fp32 in 400 481,
+// 444 and 450; in place 581 and, in the norm's order, 590.
 template <bool NT>
 __global__ __launch_bounds__(BLOCK) void k_clip_scale(const TensorList t, const double* __restrict__ part,
                                                       int64_t parts, double max_norm, double* __restrict__ norm) {

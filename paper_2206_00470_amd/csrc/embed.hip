@@ -80,9 +80,10 @@ int log_fold(int64_t blocks) { return blocks <= 256 ? 10 : blocks < 16384 ? 4 : 
 
 // Positions of a block: fewer rows are added one after another where there are
 // not enough blocks of 16 to fill the units, which costs more partial rows.
-// Measured, with 8 and with 16: 1,021 ids of 300 floats 27.0 and 31.8 us, 8,192
-// of 768 bf16 values 51.3 and 58.1; 20,000 of 2,048 65.8 and 64.0, 300,000 of 64
-// 114 and 105, 1M of 100 floats 317 and 302.
+// Measured, with 8 and with 16: 1,021 ids of 300 floats 20.9 and 24.2 us, 8,192
+// of 768 bf16 values 44.9 and 47.3 (but 400,000 of 16 floats over 1,000 rows 69
+// and 64); 20,000 of 2,048 63.6 and 55.0, 300,000 of 64 95 and 85, 1M of 100
+// floats 270 and 255.
 int log_block(int64_t n, int dim) { return n * int64_t(dim) < (int64_t(1) << 24) ? 3 : 4; }
 
 struct GradPlan {

@@ -158,17 +158,20 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__
 //
 // The codes are staged in LDS eight blocks of a row at a time, copied there
 // without a detour through registers: read straight from memory, the fragments
-// of one instruction lie in 32 lines (2,048 x 131,072 of dim 512 326 us against
-// 136). One buffer: other workgroups of the compute unit fill the wait better
+// of one instruction lie in 32 lines (2,048 x 131,072 of dim 512 326 us, staged
+// 153).  One buffer: other workgroups of the compute unit fill the wait better
 // than a second buffer does, which leaves room for two of them instead of four
-// (200 us; with registers for three 146).
+// (200 us against 153; four instead of three 136 against 146).  The scales pass
+// through LDS too, each row's brought by one thread: a lane that reads those it
+// needs asks for twice as many lines as the codes have (dim 2,048, 2,048 x 31,000:
+// 127 us against 98; dim 512 143 against 133).
 //
 // Bound by C's bytes where there are many queries (a table's width is a few
 // hundred: 2 dim operations per element written), by B's where there are few.
-// Measured: one query x 4.6M rows of 256 108 us, 6.0 TB/s of rows read and
-// scores written; 2,048 x 131,072 of dim 64 in bf16 99 us, 5.5 TB/s, of dim 512
-// 136 us, 4.2 TB/s and 2,000 TFLOP/s; 2,048 x 31,000 of dim 2,048 117 us, 2,200
-// TFLOP/s.
+// Measured: one query x 4.6M rows of 256 110 us, 5.8 TB/s of rows read and
+// scores written; 2,048 x 131,072 in bf16 of dim 64 105 us, 5.1 TB/s, of dim 512
+// 133 to 144 us, 4.1 TB/s and 2,000 TFLOP/s; 2,048 x 31,000 of dim 2,048 100 us,
+// 2,600 TFLOP/s.
 typedef int mx_operand __attribute__((ext_vector_type(8)));
 typedef float mx_acc __attribute__((ext_vector_type(16)));
 
@@ -253,7 +256,7 @@ __device__ __forceinline__ mx_operand mx_words(const words4& c) {
 // neighbouring tiles' rows meet are put together there, and the tiles at work
 // lie side by side (tiles under each other, 2^k bytes apart, meet in few
 // channels of the memory).  Measured, 2,048 x 131,072 of dim 64 and 512, bf16:
-// tiles under each other 134 and 160 us, groups 99 and 157.
+// tiles under each other 128 and 152 us, groups 105 and 144.
 constexpr uint32_t MX_GROUP = 16;
 
 // (tiles are counted in 32 bits, as workgroups are)
