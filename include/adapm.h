@@ -445,12 +445,18 @@ ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad,
 /* The same gradient as merged rows, for tables much larger than a batch:
  * uniq (device int64[n]) receives the distinct ids that take part in
  * ascending order, rows (device [n][dim], row stride rows_stride) their
- * gradient rows, *num_unique (device int32) their number U; uniq[U..] and
- * rows[U..] are left as they are.  ps_push takes uniq and rows as they are
- * (fp32, dense). */
+ * gradient rows, *num_unique (device int32, or pinned host memory) their
+ * number U, written once, before the rows are; uniq[U..] and rows[U..] are
+ * left as they are.  ps_push takes uniq and rows as they are (fp32, dense). */
 ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
                              const void* dout, int64_t dout_stride, int32_t out_type, int64_t* uniq, void* rows,
                              int64_t rows_stride, int32_t* num_unique, void* ws, size_t ws_bytes, void* stream);
+
+/* Waits on the host for a number that a call above writes to pinned host
+ * memory: until *count is not negative.  Set it to a negative number before
+ * that call.  PS_ERR_INVALID where the stream's work ends and leaves it so.
+ * Not during a capture of the stream. */
+ps_status ps_wait_count(const int32_t* count, void* stream);
 
 /* Global gradient norm of `count` tensors, and clipping by it:
  *   *norm = sqrt( sum over all tensors k and elements j of grads[k][j]^2 )

@@ -267,4 +267,24 @@ ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t
                     ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
+ps_status ps_wait_count(const int32_t* count, void* stream) {
+  if (!count) return raise(PS_ERR_INVALID, "count is NULL");
+  // (the stream is asked seldom, some 30 us apart: the number is mostly there before)
+  for (uint32_t i = 1; __atomic_load_n(count, __ATOMIC_ACQUIRE) < 0; ++i) {
+    if (i % 1024 != 0) {
+      __builtin_ia32_pause();
+      continue;
+    }
+    const hipError_t e = hipStreamQuery(static_cast<hipStream_t>(stream));
+    if (e == hipErrorNotReady) {
+      (void)hipGetLastError();   // no error, and none that a later call should report
+      continue;
+    }
+    RAISE_HIP(e);
+    if (__atomic_load_n(count, __ATOMIC_ACQUIRE) < 0)
+      return raise(PS_ERR_INVALID, "the stream is through and count is still negative");
+  }
+  return PS_OK;
+}
+
 }  // extern "C"

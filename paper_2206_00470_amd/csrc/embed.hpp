@@ -116,6 +116,11 @@ __device__ __forceinline__ void write_grad_any(const GradOut& o, int64_t row, in
   write_row_any<VW>(o, row, col, y);
 }
 
+// The number of runs, for a host that reads it while the rows are being written.
+__device__ __forceinline__ void write_count(int32_t* num_unique, int32_t u) {
+  __hip_atomic_store(num_unique, u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+
 // The runs of the sorted keys, for the rows form of calls whose sort does not
 // give them: tiles of RUNS_TILE positions count the runs that start in them;
 // then every tile adds up the counts before its own and writes its runs' keys
@@ -188,10 +193,10 @@ __global__ __launch_bounds__(BLOCK) void k_runs_write(const uint32_t* __restrict
     }
     if (k[i] < sentinel && k[i + 1] >= sentinel) {   // the last position of the last run
       seg_off[u] = (int32_t)(p + i) + 1;
-      *num_unique = (int32_t)u;
+      write_count(num_unique, (int32_t)u);
     }
   }
-  if (p == 0 && k[0] >= sentinel) *num_unique = 0;
+  if (p == 0 && k[0] >= sentinel) write_count(num_unique, 0);
 }
 
 // Index of the run that holds sorted position p, the last u with
@@ -266,7 +271,7 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
   const int count = g.n - p0 < BLK ? (int)(g.n - p0) : BLK;
   const uint32_t first = m.key[0], last = m.key[count - 1], next = m.key[count];
   if (g.seg_off && !g.block_run) {
-    if (b == 0 && slice == 0 && gl == 0) *g.num_unique = (int32_t)g.hdr->num_unique;
+    if (b == 0 && slice == 0 && gl == 0) write_count(g.num_unique, (int32_t)g.hdr->num_unique);
     // (before the rows are asked for: behind them its loads would wait for them)
     u = run_at(g.seg_off, (int32_t)g.hdr->num_unique, (int32_t)p0, lanes, gl);
   }

@@ -350,19 +350,24 @@ class Store:
                         dtype: torch.dtype = torch.float32, stream=None):
         """The same gradient as merged rows: (uniq, rows), the distinct ids in
         ascending order and their gradient rows, as push takes them.  Waits
-        for the number of distinct ids."""
+        for the number of distinct ids, not for the rows: they belong to the
+        call's stream."""
         with _On(self.W.device, stream, (ids, dout)) as st:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("embed_grad_rows waits for the number of rows: not during a capture")
             n, ld, kind, ws = self._grad_args(ids, dout)
             uniq = torch.empty(n, dtype=torch.int64, device=self.W.device)
             rows = torch.empty((n, self.dim), dtype=dtype, device=self.W.device)
             # the number comes straight to host memory: no copy to wait for behind the kernels
             count = torch.empty(1, dtype=torch.int32, pin_memory=True)
+            number = C.c_int32.from_address(count.data_ptr())
+            number.value = -1
             # (rows: an address even where there are no ids)
             check(lib().ps_embed_grad_rows(self._h, ids.data_ptr(), n, _pad(pad), scale, kind, dout.data_ptr(), ld,
                                            _type(dtype, "dtype"), uniq.data_ptr(), (rows if n else count).data_ptr(),
                                            self.dim, count.data_ptr(), ws.data_ptr(), ws.numel(), st))
-            torch.cuda.current_stream(self.W.device).synchronize()
-            U = int(count)
+            check(lib().ps_wait_count(count.data_ptr(), st))
+            U = number.value
         return uniq[:U], rows[:U]
 
     # ---------------------------------------------------------------- task steps

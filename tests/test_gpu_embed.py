@@ -441,3 +441,53 @@ def test_lookup_and_gradient_on_another_stream():
     side.synchronize()
     assert np.array_equal(bits(a), bits(a2)) and np.array_equal(bits(b), bits(b2)) and np.array_equal(bits(r), bits(r2))
     assert torch.equal(u, u2)
+
+
+@pytest.mark.parametrize("n", [1, 700, 8192, 8193, 60_000])
+def test_rows_are_used_before_they_are_finished(n):
+    """The call returns with the number of rows; what follows on the stream sees
+    the rows, whatever the stream has to do before and in between."""
+    K, d = 4000, 96
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    a = torch.randn((4096, 4096), device="cuda")
+    calls = []
+    for k in range(6):
+        ids, dout = make_ids(K, n, 300 + k), torch.randn((n, d), generator=torch.Generator().manual_seed(k))
+        calls.append((ids, dout, ids.cuda(), dout.cuda()))
+    got = []
+    for ids, dout, di, dd in calls:
+        for _ in range(3):
+            b = a @ a                                      # the stream is behind
+        u, r = s.embed_grad_rows(di, dd, pad=7)
+        got.append((u.clone(), r * 2.0))                   # read at once, and its memory used again
+        del u, r
+    for (ids, dout, _, _), (u, r) in zip(calls, got):
+        ref, mag, count = plain_grad(K, ids, dout, 1.0, 7)
+        assert torch.equal(u.cpu(), torch.nonzero(count > 0).reshape(-1))
+        check_grad(r * 0.5, ref[count > 0], mag[count > 0], count[count > 0], F32)
+    assert s.error() == 0
+
+
+def test_wait_for_the_number_of_rows():
+    K, d, n = 500, 8, 100
+    W = torch.zeros((K, d), device="cuda")
+    s = Store(W, torch.ones_like(W))
+    L, st = _lib.lib(), torch.cuda.current_stream().cuda_stream
+    count = torch.full((1,), -1, dtype=torch.int32).pin_memory()
+    # nothing writes it, with a stream that is through and with one at work
+    assert L.ps_wait_count(count.data_ptr(), st) == _lib.PS_ERR_INVALID
+    a = torch.randn((8192, 8192), device="cuda")
+    b = a @ a
+    assert L.ps_wait_count(count.data_ptr(), st) == _lib.PS_ERR_INVALID and b"negative" in L.ps_last_error_message()
+    torch.cuda.synchronize()                               # and no error is left behind
+    ids, dout = make_ids(K, n, 400).cuda(), torch.randn((n, d), device="cuda")
+    s.embed_grad_rows(ids, dout)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(RuntimeError, match="capture"):
+            s.embed_grad_rows(ids, dout)
+        x = dout * 2.0
+    g.replay()
+    assert torch.equal(x, dout * 2.0)

@@ -23,6 +23,8 @@ def test_null_store_is_refused():
     assert L.ps_embed_grad_rows(None, P(), 1, NOPAD, 1.0, F32, P(), 8, F32, P(), P(), 8, P(), P(), 1 << 20, None) == BAD
     assert L.ps_embed_grad_rows(None, P(), 1, NOPAD, 1.0, F32, P(), 8, F32, P(), P(), 8, None, P(), 1 << 20,
                                 None) == BAD
+    assert L.ps_wait_count(None, None) == BAD
+    assert L.ps_wait_count(C.byref(C.c_int32(3)), None) == 0     # there already: no stream is asked
 
 
 def test_workspace_sizes():
