@@ -16,6 +16,7 @@ struct KeysPadded {
   __device__ int64_t operator()(int64_t i) const {
     if (counter && i == 0) *counter = 0u;
     const int64_t id = ids[i];
+    if (id == ABSENT) return -1;   // as a pad it says that there is none, as an id it is outside
     return id == pad ? ABSENT : id;
   }
 };

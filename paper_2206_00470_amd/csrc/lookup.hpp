@@ -39,7 +39,7 @@ struct LookupIds {
 __device__ __forceinline__ int64_t lookup_row(const LookupIds& l, int64_t i, int& bad, int& miss) {
   if (!l.ids) return i;
   const int64_t id = l.ids[i];
-  if (id == l.pad) return -1;
+  if (id == l.pad && id != INT64_MIN) return -1;   // (INT64_MIN: there is none)
   if (id < 0 || id >= (l.map ? l.map_keys : l.num_rows)) {
     bad = 1;
     return -1;

@@ -27,7 +27,8 @@ def _dense(t: torch.Tensor, device, name: str):
 class ClipPlan:
     """The gradients of a model as one list, for its global norm and for
     clipping by it: checked and marshalled once, for buffers that stay where
-    they are from step to step.  The plan keeps the tensors.
+    they are from step to step.  The plan keeps the tensors; a call after one
+    was moved raises.
 
     grads: contiguous CUDA tensors (float32, bfloat16, float16, mixed, of any
     size) of one device.  out: where clipped gradients go, one tensor of the
@@ -53,7 +54,13 @@ class ClipPlan:
         self._numel = (C.c_int64 * k)(*(g.numel() for g in grads))
         self._in = (C.c_void_p * k)(*(g.data_ptr() for g in grads))
         self._out = (C.c_void_p * k)(*(o.data_ptr() for o in out))
+        self._at, self._out_at = list(self._in), list(self._out) if out is not grads else None
         self._words = int(lib().ps_clip_workspace_bytes(k)) // 8
+
+    def _check(self, out_at=None):
+        if [g.data_ptr() or None for g in self.grads] != self._at or (
+                out_at is not None and [o.data_ptr() or None for o in self.out] != out_at):
+            raise RuntimeError("a tensor of the plan has moved: make a new one")
 
     def _buffers(self):
         # of its own per call: a captured call keeps the ones it was captured with
@@ -62,6 +69,7 @@ class ClipPlan:
 
     def norm(self, stream=None) -> torch.Tensor:
         """The global norm of the gradients, float64[1]."""
+        self._check()
         with _On(self.device, stream, self.grads) as st:
             norm, ws, wsb = self._buffers()
             check(lib().ps_grad_norm(self._n, self._in, self._numel, self._types, norm.data_ptr(), ws, wsb, st))
@@ -70,6 +78,7 @@ class ClipPlan:
     def clip(self, max_norm: float, stream=None) -> torch.Tensor:
         """Write the gradients, scaled by max_norm / norm where the norm is
         larger, to the outputs; returns the norm before, float64[1]."""
+        self._check(self._out_at)
         with _On(self.device, stream, (*self.grads, *self.out) if stream is not None else ()) as st:
             norm, ws, wsb = self._buffers()
             check(lib().ps_clip_grads(self._n, self._in, self._out, self._numel, self._types, max_norm,
@@ -137,6 +146,7 @@ class MX4:
                 if torch.cuda.is_current_stream_capturing():
                     raise RuntimeError("the first embed of a table makes its error flag: call it before a capture")
                 self._err = torch.zeros(2, dtype=torch.int32, device=self.device)
+                torch.cuda.current_stream(self.device).synchronize()   # zero for calls on every stream
             ld = self.dim
             if out is None:
                 out = torch.empty((*shape, ld), dtype=dtype, device=self.device)
@@ -151,9 +161,11 @@ class MX4:
 
     def error(self) -> int:
         """Synchronize, then return and clear the sticky status of embed."""
+        torch.cuda.synchronize(self.device)
         if self._err is None or not int(self._err[0].item()):
             return _lib.PS_OK
         self._err.zero_()
+        torch.cuda.synchronize(self.device)
         return _lib.PS_ERR_KEY_RANGE
 
 

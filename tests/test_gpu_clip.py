@@ -219,3 +219,20 @@ def test_a_training_step_of_a_token_table():
     step = lr * gd / Gd.sqrt()
     assert float((W.cpu().double() - (Wd - step)).abs().max()) <= tol * float(step.abs().max()) + 2.0 ** -23 * float(Wd.abs().max())
     assert torch.equal(uniq.cpu(), torch.unique(ids[ok]))
+
+
+def test_a_plan_whose_tensors_moved_is_refused():
+    grads = [torch.randn(n, device="cuda") for n in (100, 20_000)]
+    outs = [torch.empty_like(g) for g in grads]
+    plan, inplace = ClipPlan(grads, outs), ClipPlan(grads)
+    plan.clip(1.0)
+    old = grads[1].data
+    grads[1].data = torch.randn(20_000, device="cuda")
+    for call in (plan.norm, inplace.norm, lambda: plan.clip(1.0), lambda: inplace.clip(1.0)):
+        with pytest.raises(RuntimeError, match="moved"):
+            call()
+    grads[1].data = old
+    outs[0].data = torch.empty(100, device="cuda")
+    with pytest.raises(RuntimeError, match="moved"):
+        plan.clip(1.0)
+    plan.norm(), inplace.clip(1.0)

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2206_00470_amd import StagedStore, Store, _lib
+from paper_2206_00470_amd import StagedStore, Store, _lib, mx4_quantize
 from paper_2206_00470_amd._lib import PSError
 from paper_2206_00470_amd.store import interleaved_bf16_tables, interleaved_tables, padded_rowwise_table
 from tests.helpers import say
@@ -491,3 +491,26 @@ def test_wait_for_the_number_of_rows():
         x = dout * 2.0
     g.replay()
     assert torch.equal(x, dout * 2.0)
+
+
+@pytest.mark.parametrize("n", [5, 9000])
+@pytest.mark.parametrize("pad", [None, 4])
+def test_the_lowest_id_is_outside_the_table(n, pad):
+    """INT64_MIN says "no padding" as an argument; as an id it is one outside."""
+    K, d = 40, 12
+    W = table(K, d, 90).cuda()
+    s = Store(W, torch.ones_like(W))
+    ids = make_ids(K, n, 91)
+    ids[n // 2] = -(1 << 63)
+    dout = torch.randn((n, d), generator=torch.Generator().manual_seed(92))
+    assert np.array_equal(bits(s.embed(ids.cuda(), pad=pad)), bits(plain_embed(W.cpu(), ids, 1.0, F32, pad)))
+    assert s.error() == _lib.PS_ERR_KEY_RANGE
+    check_grad(s.embed_grad(ids.cuda(), dout.cuda(), pad=pad), *plain_grad(K, ids, dout, 1.0, pad), F32)
+    assert s.error() == _lib.PS_ERR_KEY_RANGE
+    u, r = s.embed_grad_rows(ids.cuda(), dout.cuda(), pad=pad)
+    ref, mag, count = plain_grad(K, ids, dout, 1.0, pad)
+    check_grad(r, ref[count > 0], mag[count > 0], count[count > 0], F32)
+    assert s.error() == _lib.PS_ERR_KEY_RANGE
+    x = mx4_quantize(W)
+    got = x.embed(ids.cuda(), pad=pad)
+    assert bool((got[n // 2] == 0).all()) and x.error() == _lib.PS_ERR_KEY_RANGE and x.error() == 0

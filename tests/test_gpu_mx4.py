@@ -262,3 +262,20 @@ def test_a_quantised_table_answers():
     queries = mx4_quantize(q.embed(ids, dtype=BF16))
     score = check_product(queries, q, F32, 128 ** -0.5)
     assert torch.equal(score.argmax(dim=1), ids)
+
+
+def test_a_table_used_first_on_two_streams_reports_its_error():
+    """The flag that embed makes at its first call is there for every stream."""
+    x = mx4_quantize(torch.randn((50, 64), device="cuda"))
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    good, bad = torch.arange(50, device="cuda"), torch.full((3,), 50, dtype=torch.int64, device="cuda")
+    torch.cuda.synchronize()
+    a = torch.randn((8192, 8192), device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(one):
+        b = a @ a                      # the first call's stream is behind
+    x.embed(good, stream=one)
+    x.embed(bad, stream=two)
+    torch.cuda.synchronize()
+    assert x.error() == _lib.PS_ERR_KEY_RANGE and x.error() == 0
