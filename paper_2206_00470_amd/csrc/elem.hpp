@@ -54,6 +54,17 @@ __device__ __forceinline__ uint32_t narrow_word(f16_t, float f) {
   return __builtin_bit_cast(uint16_t, (f16_t)f);
 }
 
+// Two values in a word, the first in the low half.
+typedef float float_pair __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t narrow_pair(bf16_t, float a, float b) {   // one instruction
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((float_pair{a, b}), bf16_pair));
+}
+__device__ __forceinline__ uint32_t narrow_pair(f16_t, float a, float b) {
+  return narrow_word(f16_t{}, a) | narrow_word(f16_t{}, b) << 16;
+}
+
 template <class T, int VW>
 __device__ __forceinline__ raw_t<T, VW> raw_make(const float* x) {
   if constexpr (std::is_same_v<T, float>) {
@@ -70,7 +81,7 @@ __device__ __forceinline__ raw_t<T, VW> raw_make(const float* x) {
   } else {
     raw_t<T, VW> r;
 #pragma unroll
-    for (int e = 0; e < VW; e += 2) r[e / 2] = narrow_word(T{}, x[e]) | narrow_word(T{}, x[e + 1]) << 16;
+    for (int e = 0; e < VW; e += 2) r[e / 2] = narrow_pair(T{}, x[e], x[e + 1]);
     return r;
   }
 }
