@@ -47,7 +47,7 @@ ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, floa
   // stores of 16 bytes (to bf16 from fp32 in vectors of four: 105 us instead of 89 as in lookup.hpp)
   const int vw = t.dim >= 8 && ob == 2 ? 8 : t.dim >= 4 ? 4 : 1;
   const SmallDiv nv = small_div((uint32_t)div_up(t.dim, vw));
-  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * EMBED_FLIGHT);
+  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * LOOKUP_FLIGHT);
   if (grid > GRID_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the lookup's grid", (long long)n, t.dim);
   const LookupIds l{ids, n, pad, t.num_keys, t.map, t.map_keys, t.status};
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {

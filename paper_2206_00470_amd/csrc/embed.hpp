@@ -10,7 +10,7 @@ namespace adapm {
 //   out[i] = T( scale * W[ids[i]] ),   zero where ids[i] == pad
 // (the product is rounded to fp32, then to T).  Bound by the rows read and
 // written.  The rows are cut into vectors of VW elements and the vectors of
-// the whole output dealt out in order, EMBED_FLIGHT in flight per thread: every
+// the whole output dealt out in order, LOOKUP_FLIGHT in flight per thread: every
 // lane has a vector whatever the row's width, a row of any width is spread
 // over as many workgroups as it fills, and a workgroup writes one stretch.  A
 // row that is no multiple of VW has its last vector end with the row, over some
@@ -18,7 +18,7 @@ namespace adapm {
 template <class VT, class OT, int VW, bool NT>
 __global__ __launch_bounds__(BLOCK) void k_embed(const VT* __restrict__ W, int64_t ld, LookupIds l, SmallDiv nv,
                                                  int dim, float scale, OT* __restrict__ out, int64_t out_ld) {
-  constexpr int U = EMBED_FLIGHT;
+  constexpr int U = LOOKUP_FLIGHT;
   const int64_t q0 = (int64_t)blockIdx.x * (BLOCK * U);
   const int64_t row0 = row_of(q0, nv.d);
   const uint32_t first = (uint32_t)(q0 - row0 * nv.d) + threadIdx.x;

@@ -5,18 +5,16 @@
 
 namespace adapm {
 
-// Vectors in flight per thread, of an fp32 or bf16 table and of a 4-bit one,
-// whose address takes longer to work out: 65,536 rows of 2,048 floats to bf16
-// 106 us with four, 89 with two or one; a table of 4.6M x 256 4-bit values
-// restored to bf16 587 with one, 516 with two, 491 with four.
-constexpr int EMBED_FLIGHT = 2;
-constexpr int MX4_FLIGHT = 4;
+// Vectors in flight per thread: 65,536 rows of 2,048 floats to bf16 106 us with
+// four, 89 with two or one; a table of 4.6M x 256 4-bit values restored to bf16
+// 483 with four, 470 with two, 554 with one.
+constexpr int LOOKUP_FLIGHT = 2;
 
 // Outputs beyond this are written past the caches. Measured, through them and
 // past them, a lookup alone and with a kernel behind it that reads the output:
 // 61 MB (rows of 512 floats to bf16) 24.7 and 21.6 us, 47.2 and 48.9; 85 MB (100
-// floats) 33.0 and 23.5, 60.5 and 61.0; 127 MB (300 4-bit values to bf16) 50.6
-// and 33.1, 95.4 and 87.4; 240 MB (301 floats) 96.8 and 57.5, 178 and 164.
+// floats) 30.9 and 22.5, 57.3 and 58.7; 127 MB (300 4-bit values to bf16) 49.2
+// and 29.2, 93.7 and 85.7; 240 MB (301 floats) 90.7 and 57.1, 172 and 156.
 constexpr int64_t LOOKUP_STREAMS = int64_t(80) << 20;
 
 // The row of vector q, d vectors a row (a 64-bit division takes several times as

@@ -71,7 +71,7 @@ ps_status ps_mx4_embed(const uint8_t* codes, const uint8_t* scales, int64_t num_
   if (!on_bytes(out, b)) return raise(PS_ERR_INVALID, "out is not aligned to its elements");
   const SmallDiv nv = small_div((uint32_t)div_up(dim, 16 / b));
   if (n > INT64_MAX / (4 * nv.d)) return raise(PS_ERR_UNSUPPORTED, "%lld rows", (long long)n);
-  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * MX4_FLIGHT);
+  const int64_t grid = div_up(n * nv.d, int64_t(BLOCK) * LOOKUP_FLIGHT);
   if (grid > GRID_MAX) return raise(PS_ERR_UNSUPPORTED, "%lld rows of %d exceed the grid", (long long)n, dim);
   const LookupIds l{ids, n, pad, num_rows, nullptr, 0, err};
   return with_type(out_type, [&]<class OT>(OT) -> ps_status {
