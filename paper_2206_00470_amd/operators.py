@@ -54,12 +54,13 @@ class ClipPlan:
         self._numel = (C.c_int64 * k)(*(g.numel() for g in grads))
         self._in = (C.c_void_p * k)(*(g.data_ptr() for g in grads))
         self._out = (C.c_void_p * k)(*(o.data_ptr() for o in out))
-        self._at, self._out_at = list(self._in), list(self._out) if out is not grads else None
+        self._at = [g.data_ptr() for g in grads]
+        self._out_at = [o.data_ptr() for o in out] if out is not grads else None
         self._words = int(lib().ps_clip_workspace_bytes(k)) // 8
 
     def _check(self, out_at=None):
-        if [g.data_ptr() or None for g in self.grads] != self._at or (
-                out_at is not None and [o.data_ptr() or None for o in self.out] != out_at):
+        if list(map(torch.Tensor.data_ptr, self.grads)) != self._at or (
+                out_at is not None and list(map(torch.Tensor.data_ptr, self.out)) != out_at):
             raise RuntimeError("a tensor of the plan has moved: make a new one")
 
     def _buffers(self):
