@@ -115,12 +115,21 @@ ps_status ps_mx4_product(int64_t m, int64_t n, int32_t dim, const uint8_t* a_cod
     // past the caches where C fills the last-level one and its rows are whole lines
     // (1,024 x 65,536 in fp32 of dim 1,024 108 us through the caches, 77 past them;
     // rows that share lines, 2,048 x 50,021 in fp32 131 and 173)
-    const bool nt = m * n * (int64_t)sizeof(OT) >= LLC_BYTES && on_bytes(out, 64) && out_stride * sizeof(OT) % 64 == 0;
+    const int64_t bytes = m * n * (int64_t)sizeof(OT);
+    const bool lines = on_bytes(out, 64) && out_stride * sizeof(OT) % 64 == 0, nt = bytes >= LLC_BYTES && lines;
     if (m <= 32) {
       if (nt) return launch(k_mx4_product<OT, 1, 2, 1, 4, true>, 32, 256);
       return launch(k_mx4_product<OT, 1, 2, 1, 4, false>, 32, 256);
     }
     if (nt) return launch(k_mx4_product<OT, 2, 2, 2, 2, true>, 128, 128);
+    // rows that share lines, many and long: wider tiles share fewer, and cost more
+    // loads, which count where rows are wide (tiles of 128 x 128 and 64 x 256, us:
+    // 2,048 x 100,043 in bf16 of dim 64, 300 and 512 130 and 106, 143 and 133, 149
+    // and 148, 2,048 x 20,011 of 256 35 and 23, 256 x 300,003 in fp32 of 256 101 and
+    // 91; but 2,048 x 50,021 in bf16 of 2,048 157 and 185, 200 x 100,003 in fp32 of
+    // 128 17.4 and 18.2, 2,048 x 10,007 in bf16 of 64 12.7 and 13.7)
+    if (!lines && bytes >= LLC_BYTES / 4 && m >= 256 && dim <= 512)
+      return launch(k_mx4_product<OT, 2, 2, 1, 4, false>, 64, 256);
     return launch(k_mx4_product<OT, 2, 2, 2, 2, false>, 128, 128);
   });
 }

@@ -285,8 +285,9 @@ __device__ __forceinline__ void mx_tile(uint32_t tiles_q, uint32_t tiles_b, uint
 
 // A wave's tile is QT x 32 rows of A by TT x 32 rows of B; a workgroup's waves
 // stand WQ x WT.  Rows of C are stored 16 bytes at a time wherever they start.
+// Four workgroups stand in a compute unit, three of the widest tile (by their LDS).
 template <class OT, int QT, int TT, int WQ, int WT, bool NT>
-__global__ __launch_bounds__(BLOCK, 4) void k_mx4_product(MxRows A, MxRows B, int blocks_row, float scale,
+__global__ __launch_bounds__(BLOCK, WQ * QT + WT * TT <= 9 ? 4 : 3) void k_mx4_product(MxRows A, MxRows B, int blocks_row, float scale,
                                                        OT* __restrict__ C, int64_t ldc, uint32_t tiles_q,
                                                        uint32_t tiles_b) {
   constexpr int VW = 16 / sizeof(OT);

@@ -253,6 +253,27 @@ def test_product_strides_special_scales_and_order():
         mx4_product(q, t, out=torch.empty((300, 701), device="cuda"))
 
 
+@pytest.mark.parametrize("m,n,dim,dtype,off", [
+    (256, 65_601, 100, F32, 0), (256, 65_601, 100, F32, 3), (259, 131_201, 512, BF16, 0), (300, 120_001, 513, BF16, 0),
+    (513, 70_001, 31, F16, 1), (255, 65_901, 64, F32, 0), (2048, 32_768, 64, F32, 0), (2049, 65_600, 33, BF16, 0),
+    (2049, 65_601, 300, BF16, 0)])
+def test_products_of_every_size_have_the_same_scores(m, n, dim, dtype, off):
+    """Large results, their rows whole cache lines or not: the scores are those
+    of a few queries at a time (which are checked against 64 bits), and what
+    lies around the result stays."""
+    say(f"product {m} x {n} x {dim} {dtype}")
+    a, b = random_mx4(m, dim, 21), random_mx4(n, dim, 22)
+    room = torch.full((m * n + off + 64,), 7.0, dtype=dtype, device="cuda")
+    out = room[off:off + m * n].view(m, n)
+    mx4_product(a, b, scale=2.0 ** -9, out=out)
+    assert bool((room[:off] == 7.0).all()) and bool((room[off + m * n:] == 7.0).all())
+    for i in (0, 32, m // 2, m - 20):
+        q = MX4(a.codes[i:i + 20].contiguous(), a.scales[i:i + 20].contiguous(), dim)
+        assert torch.equal(mx4_product(q, b, scale=2.0 ** -9, dtype=dtype), out[i:i + 20])
+    few = MX4(b.codes[n - 40:].contiguous(), b.scales[n - 40:].contiguous(), dim)
+    assert torch.equal(check_product(a, few, dtype, 2.0 ** -9), out[:, n - 40:])
+
+
 def test_a_quantised_table_answers():
     """Scores of a table's own rows: quantise, look queries up, quantise them,
     score them against all rows; each row's best score is its own."""
