@@ -479,6 +479,19 @@ ps_status ps_grad_norm(int32_t count, const void* const* grads, const int64_t* n
 ps_status ps_clip_grads(int32_t count, const void* const* grads, void* const* outs, const int64_t* numel,
                         const int32_t* types, double max_norm, double* norm, void* ws, size_t ws_bytes, void* stream);
 
+/* The same for tensors that stay where they are from call to call: a list of
+ * them, made once.  ps_clip_plan checks the tensors and writes ps_clip_plan_bytes
+ * (0: none, or invalid arguments) to host memory `plan`, and to *apart (host) the
+ * bytes that clipping writes apart from what it reads.  The caller copies the
+ * plan to device memory (8-byte aligned), which ps_clip_run takes; it must stay
+ * there while calls, or captured graphs of them, may run.  scaling 0: the norm
+ * alone.  Workspace: ps_clip_workspace_bytes(1). */
+size_t ps_clip_plan_bytes(int32_t count, const int64_t* numel);
+ps_status ps_clip_plan(int32_t count, const void* const* grads, void* const* outs, const int64_t* numel,
+                       const int32_t* types, void* plan, size_t plan_bytes, int64_t* apart);
+ps_status ps_clip_run(const void* plan, size_t plan_bytes, int64_t apart, int32_t scaling, double max_norm,
+                      double* norm, void* ws, size_t ws_bytes, void* stream);
+
 /* Microscaled 4-bit rows: each row of dim values in ceil(dim/32) blocks of 32
  * (the last filled up with zeros), 16 bytes of codes and one scale byte s a
  * block.  A code is sign, two exponent bits and one mantissa bit (magnitudes

@@ -81,6 +81,9 @@ SIGNATURES = {
     "ps_clip_workspace_bytes": (_sz, [_i32]),
     "ps_grad_norm": (_i32, [_i32, _p, _p, _p, _p, _p, _sz, _p]),
     "ps_clip_grads": (_i32, [_i32, _p, _p, _p, _p, C.c_double, _p, _p, _sz, _p]),
+    "ps_clip_plan_bytes": (_sz, [_i32, _p]),
+    "ps_clip_plan": (_i32, [_i32, _p, _p, _p, _p, _p, _sz, _p]),
+    "ps_clip_run": (_i32, [_p, _sz, _i64, _i32, C.c_double, _p, _p, _sz, _p]),
     "ps_mx4_quantize": (_i32, [_i64, _i32, _i32, _p, _i64, _p, _p, _p]),
     "ps_mx4_embed": (_i32, [_p, _p, _i64, _i32, _p, _i64, _i64, _f32, _i32, _p, _i64, _p, _p]),
     "ps_mx4_product": (_i32, [_i64, _i64, _i32, _p, _p, _p, _p, _f32, _i32, _p, _i64, _p]),

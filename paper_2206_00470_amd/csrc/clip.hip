@@ -2,6 +2,7 @@
 #include "clip.hpp"
 
 #include <algorithm>
+#include <cstring>
 #include <new>
 #include <vector>
 
@@ -66,16 +67,29 @@ ps_status check_tensors(int32_t count, const void* const* grads, void* const* ou
   return PS_OK;
 }
 
-ps_status clip(int32_t count, const void* const* grads, void* const* outs, const int64_t* numel, const int32_t* types,
-               double max_norm, double* norm, void* ws, size_t ws_bytes, hipStream_t st) {
-  if (ps_status r = check_tensors(count, grads, outs, numel, types)) return r;
+ps_status check_call(bool scaling, double max_norm, double* norm, void* ws, size_t ws_bytes, size_t need) {
   if (!norm) return raise(PS_ERR_INVALID, "norm is NULL");
   if (!on_bytes(norm, 8)) return raise(PS_ERR_INVALID, "norm is not aligned to its elements");
-  if (outs && !(max_norm > 0.0)) return raise(PS_ERR_INVALID, "need max_norm > 0");
-  const size_t need = ps_clip_workspace_bytes(count);
+  if (scaling && !(max_norm > 0.0)) return raise(PS_ERR_INVALID, "need max_norm > 0");
   if (!ws) return raise(PS_ERR_INVALID, "workspace pointer is NULL");
   if (ws_bytes < need) return raise(PS_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
   if (!on_bytes(ws, 8)) return raise(PS_ERR_INVALID, "the workspace must be 8-byte aligned");
+  return PS_OK;
+}
+
+// Outputs of so many bytes, apart from what is read, are written past the caches.
+bool streams(int64_t apart) { return apart > LLC_BYTES / 2; }
+
+ps_status total(const double* part, int64_t parts, double* norm, hipStream_t st) {
+  hipLaunchKernelGGL(k_norm_total, dim3(1), dim3(BLOCK), 0, st, part, parts, norm);
+  RAISE_HIP(hipGetLastError());
+  return PS_OK;
+}
+
+ps_status clip(int32_t count, const void* const* grads, void* const* outs, const int64_t* numel, const int32_t* types,
+               double max_norm, double* norm, void* ws, size_t ws_bytes, hipStream_t st) {
+  if (ps_status r = check_tensors(count, grads, outs, numel, types)) return r;
+  if (ps_status r = check_call(outs, max_norm, norm, ws, ws_bytes, ps_clip_workspace_bytes(count))) return r;
   double* part = static_cast<double*>(ws);
   std::vector<TensorList> lists;
   int32_t k = 0;
@@ -97,19 +111,15 @@ ps_status clip(int32_t count, const void* const* grads, void* const* outs, const
   auto grid = [](const TensorList& t) { return std::min<int64_t>(t.first[t.count], CLIP_GRID); };
   int64_t parts = 0;
   for (const TensorList& t : lists) {
-    hipLaunchKernelGGL(k_norm_part, dim3(grid(t)), dim3(BLOCK), 0, st, t, part + parts);
+    hipLaunchKernelGGL(k_norm_part<TensorList>, dim3(grid(t)), dim3(BLOCK), 0, st, t, part + parts);
     RAISE_HIP(hipGetLastError());
     parts += grid(t);
   }
-  if (!outs || lists.empty()) {
-    hipLaunchKernelGGL(k_norm_total, dim3(1), dim3(BLOCK), 0, st, part, parts, norm);
-    RAISE_HIP(hipGetLastError());
-    return PS_OK;
-  }
-  int64_t bytes = 0;   // written apart from what is read
+  if (!outs || lists.empty()) return total(part, parts, norm, st);
+  int64_t apart = 0;
   for (int32_t i = 0; i < count; ++i)
-    if (grads[i] != outs[i]) bytes += numel[i] * type_bytes(types[i]);
-  auto kernel = bytes > LLC_BYTES / 2 ? k_clip_scale<true> : k_clip_scale<false>;
+    if (grads[i] != outs[i]) apart += numel[i] * type_bytes(types[i]);
+  auto kernel = streams(apart) ? k_clip_scale<true, TensorList> : k_clip_scale<false, TensorList>;
   for (size_t i = lists.size(); i-- > 0;) {
     hipLaunchKernelGGL(kernel, dim3(grid(lists[i])), dim3(BLOCK), 0, st, lists[i], part, parts, max_norm,
                        i == 0 ? norm : nullptr);
@@ -146,6 +156,65 @@ ps_status ps_clip_grads(int32_t count, const void* const* grads, void* const* ou
   } catch (const std::bad_alloc&) {
     return raise(PS_ERR_DEVICE, "out of host memory");
   }
+}
+
+size_t ps_clip_plan_bytes(int32_t count, const int64_t* numel) {
+  if (count < 0 || (count > 0 && !numel)) return 0;
+  int64_t chunks = 0;
+  for (int32_t k = 0; k < count; ++k) {
+    if (numel[k] < 0 || numel[k] > NUMEL_MAX) return 0;
+    chunks += div_up(numel[k], CLIP_CHUNK);
+  }
+  return size_t(chunks) * sizeof(ClipChunk);
+}
+
+ps_status ps_clip_plan(int32_t count, const void* const* grads, void* const* outs, const int64_t* numel,
+                       const int32_t* types, void* plan, size_t plan_bytes, int64_t* apart) {
+  if (count > 0 && !outs) return raise(PS_ERR_INVALID, "outs is NULL");
+  if (!apart) return raise(PS_ERR_INVALID, "apart is NULL");
+  try {
+    if (ps_status r = check_tensors(count, grads, outs, numel, types)) return r;
+    if (plan_bytes != ps_clip_plan_bytes(count, numel))
+      return raise(PS_ERR_INVALID, "the plan has %zu bytes, not %zu", plan_bytes, ps_clip_plan_bytes(count, numel));
+    if (plan_bytes / sizeof(ClipChunk) > UINT32_MAX / 2) return raise(PS_ERR_UNSUPPORTED, "%zu bytes of chunks", plan_bytes);
+    if (plan_bytes > 0 && !plan) return raise(PS_ERR_INVALID, "plan is NULL");
+    char* to = static_cast<char*>(plan);
+    *apart = 0;
+    for (int32_t k = 0; k < count; ++k) {
+      const int64_t b = type_bytes(types[k]);
+      if (grads[k] != outs[k]) *apart += numel[k] * b;
+      for (int64_t i = 0; i < numel[k]; i += CLIP_CHUNK, to += sizeof(ClipChunk)) {
+        const ClipChunk c{static_cast<const char*>(grads[k]) + i * b, static_cast<char*>(outs[k]) + i * b,
+                          (uint32_t)std::min(numel[k] - i, CLIP_CHUNK), (uint32_t)types[k]};
+        std::memcpy(to, &c, sizeof c);
+      }
+    }
+    return PS_OK;
+  } catch (const std::bad_alloc&) {
+    return raise(PS_ERR_DEVICE, "out of host memory");
+  }
+}
+
+ps_status ps_clip_run(const void* plan, size_t plan_bytes, int64_t apart, int32_t scaling, double max_norm,
+                      double* norm, void* ws, size_t ws_bytes, void* stream) {
+  if (plan_bytes % sizeof(ClipChunk) || plan_bytes / sizeof(ClipChunk) > UINT32_MAX / 2)
+    return raise(PS_ERR_INVALID, "%zu bytes are no plan", plan_bytes);
+  if (plan_bytes > 0 && (!plan || !on_bytes(plan, alignof(ClipChunk))))
+    return raise(PS_ERR_INVALID, "plan is NULL or not 8-byte aligned");
+  if (ps_status r = check_call(scaling, max_norm, norm, ws, ws_bytes, ps_clip_workspace_bytes(1))) return r;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  double* part = static_cast<double*>(ws);
+  const ChunkList t{static_cast<const ClipChunk*>(plan), (uint32_t)(plan_bytes / sizeof(ClipChunk))};
+  const uint32_t grid = std::min<uint32_t>(t.n, CLIP_GRID);
+  if (grid > 0) {
+    hipLaunchKernelGGL(k_norm_part<ChunkList>, dim3(grid), dim3(BLOCK), 0, st, t, part);
+    RAISE_HIP(hipGetLastError());
+  }
+  if (!scaling || grid == 0) return total(part, grid, norm, st);
+  auto kernel = streams(apart) ? k_clip_scale<true, ChunkList> : k_clip_scale<false, ChunkList>;
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(BLOCK), 0, st, t, part, int64_t(grid), max_norm, norm);
+  RAISE_HIP(hipGetLastError());
+  return PS_OK;
 }
 
 }  // extern "C"

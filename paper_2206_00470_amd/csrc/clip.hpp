@@ -8,9 +8,13 @@
 // first a power of two, so that it keeps its 24 bits.
 //
 // The tensors are cut into chunks of CLIP_CHUNK elements and the chunks of all
-// of them dealt out over one grid.  A launch carries its tensors' addresses in
-// its arguments, CLIP_TENSORS at a time: nothing is copied to the device and a
-// captured launch holds its own list.  Each workgroup of the norm leaves one
+// of them dealt out over one grid.  A plan has a list of its chunks in device
+// memory: one launch for the norm and one for the scaling, however many tensors
+// there are.  A call without a plan carries its tensors' addresses in the
+// launches' arguments, CLIP_TENSORS at a time: nothing is copied to the device
+// (a call on 397 tensors of 26,610 floats in all 43 us with a plan, 75 without, on
+// 291 of 500M bf16 values 518 and 525).
+// Each workgroup of the norm leaves one
 // partial sum; each workgroup of the scaling adds all of them up again by
 // itself, in one order, instead of waiting for another launch to do so.
 #pragma once
@@ -23,6 +27,21 @@ constexpr int CLIP_TENSORS = 128;
 constexpr int64_t CLIP_CHUNK = 16384;
 constexpr int64_t CLIP_GRID = 768;   // workgroups of a launch, at most: three a compute unit
 
+// A part of a tensor.
+struct ClipChunk {
+  const void* in;
+  void* out;
+  uint32_t count;   // elements
+  uint32_t type;
+};
+
+struct ChunkList {
+  const ClipChunk* list;
+  uint32_t n;
+  __device__ __forceinline__ uint32_t chunks() const { return n; }
+  __device__ __forceinline__ ClipChunk at(uint32_t c) const { return list[c]; }
+};
+
 struct TensorList {
   const void* in[CLIP_TENSORS];
   void* out[CLIP_TENSORS];
@@ -30,18 +49,20 @@ struct TensorList {
   uint32_t first[CLIP_TENSORS + 1];   // first chunk of each tensor; the last entry: chunks in all
   uint8_t type[CLIP_TENSORS];
   int32_t count;
-};
-
-// The tensor of chunk c (uniform over the workgroup).
-__device__ __forceinline__ int tensor_of(const TensorList& t, uint32_t c) {
-  int lo = 0, hi = t.count;   // first[lo] <= c < first[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (t.first[mid] <= c) lo = mid;
-    else hi = mid;
+  __device__ __forceinline__ uint32_t chunks() const { return first[count]; }
+  __device__ __forceinline__ ClipChunk at(uint32_t c) const {   // (uniform over the workgroup)
+    int k = 0, hi = count;   // first[k] <= c < first[hi]
+    while (hi - k > 1) {
+      const int mid = (k + hi) / 2;
+      if (first[mid] <= c) k = mid;
+      else hi = mid;
+    }
+    const int64_t i0 = (int64_t)(c - first[k]) * CLIP_CHUNK, left = numel[k] - i0;
+    const int64_t byte = i0 * (type[k] == 0 ? 4 : 2);
+    return ClipChunk{static_cast<const char*>(in[k]) + byte, static_cast<char*>(out[k]) + byte,
+                     (uint32_t)(left < CLIP_CHUNK ? left : CLIP_CHUNK), type[k]};
   }
-  return lo;
-}
+};
 
 // f(p, n) over the elements [i0, i1) of a tensor: VW at a time from the first
 // address that is aligned for them, the rest one by one.
@@ -86,18 +107,16 @@ __device__ __forceinline__ double chunk_squares(const T* p, int64_t count) {
   return s0 + s1;
 }
 
-__global__ __launch_bounds__(BLOCK) void k_norm_part(const TensorList t, double* __restrict__ part) {
+template <class List>
+__global__ __launch_bounds__(BLOCK) void k_norm_part(const List t, double* __restrict__ part) {
   __shared__ double smem[WAVES_PER_BLOCK];
   double s = 0.0;
-  const uint32_t chunks = t.first[t.count];
+  const uint32_t chunks = t.chunks();
   for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const int k = tensor_of(t, c);
-    const int64_t i0 = (int64_t)(c - t.first[k]) * CLIP_CHUNK;
-    const int64_t left = t.numel[k] - i0;
-    const int64_t count = left < CLIP_CHUNK ? left : CLIP_CHUNK;
-    if (t.type[k] == 0) s += chunk_squares(static_cast<const float*>(t.in[k]) + i0, count);
-    else if (t.type[k] == 1) s += chunk_squares(static_cast<const bf16_t*>(t.in[k]) + i0, count);
-    else s += chunk_squares(static_cast<const f16_t*>(t.in[k]) + i0, count);
+    const ClipChunk x = t.at(c);
+    if (x.type == 0) s += chunk_squares(static_cast<const float*>(x.in), x.count);
+    else if (x.type == 1) s += chunk_squares(static_cast<const bf16_t*>(x.in), x.count);
+    else s += chunk_squares(static_cast<const f16_t*>(x.in), x.count);
   }
   s = block_sum_double(s, smem);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -170,13 +189,13 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* o, int64_t count, Coe
 
 // The chunks go from the last to the first: the ones read last for the norm are
 // still in the last-level cache.  NT (large outputs that are not their inputs)
-// writes past the caches.  Measured, 500M bf16 values in 291 tensors: 567 us
+// writes past the caches.  Measured without a plan, 500M bf16 values in 291 tensors: 567 us
 // through the caches, 528 past them (174 of it the norm, 5.7 TB/s read; 5.6 TB/s
 // read and written by the rest), 536 in the norm's order; 200M fp32 in 400 481,
 // 444 and 450; in place 581 and, in the norm's order, 590.
-template <bool NT>
-__global__ __launch_bounds__(BLOCK) void k_clip_scale(const TensorList t, const double* __restrict__ part,
-                                                      int64_t parts, double max_norm, double* __restrict__ norm) {
+template <bool NT, class List>
+__global__ __launch_bounds__(BLOCK) void k_clip_scale(const List t, const double* __restrict__ part, int64_t parts,
+                                                      double max_norm, double* __restrict__ norm) {
   __shared__ double smem[WAVES_PER_BLOCK];
   __shared__ double norm_sh;
   const double nm = total_norm(part, parts, smem);
@@ -186,20 +205,14 @@ __global__ __launch_bounds__(BLOCK) void k_clip_scale(const TensorList t, const 
   }
   __syncthreads();
   const Coef coef = coef_of(norm_sh, max_norm);
-  const uint32_t chunks = t.first[t.count];
+  const uint32_t chunks = t.chunks();
   for (uint32_t q = blockIdx.x; q < chunks; q += gridDim.x) {
-    const uint32_t c = chunks - 1 - q;
-    const int k = tensor_of(t, c);
-    if (coef.c == 1.0f && t.in[k] == t.out[k]) continue;   // in place, and within the bound
-    const int64_t i0 = (int64_t)(c - t.first[k]) * CLIP_CHUNK;
-    const int64_t left = t.numel[k] - i0;
-    const int64_t count = left < CLIP_CHUNK ? left : CLIP_CHUNK;
-    if (t.type[k] == 0)
-      chunk_scale<float, NT>(static_cast<const float*>(t.in[k]) + i0, static_cast<float*>(t.out[k]) + i0, count, coef);
-    else if (t.type[k] == 1)
-      chunk_scale<bf16_t, NT>(static_cast<const bf16_t*>(t.in[k]) + i0, static_cast<bf16_t*>(t.out[k]) + i0, count, coef);
-    else
-      chunk_scale<f16_t, NT>(static_cast<const f16_t*>(t.in[k]) + i0, static_cast<f16_t*>(t.out[k]) + i0, count, coef);
+    const ClipChunk x = t.at(chunks - 1 - q);
+    if (coef.c == 1.0f && x.in == x.out) continue;   // in place, and within the bound
+    if (x.type == 0) chunk_scale<float, NT>(static_cast<const float*>(x.in), static_cast<float*>(x.out), x.count, coef);
+    else if (x.type == 1)
+      chunk_scale<bf16_t, NT>(static_cast<const bf16_t*>(x.in), static_cast<bf16_t*>(x.out), x.count, coef);
+    else chunk_scale<f16_t, NT>(static_cast<const f16_t*>(x.in), static_cast<f16_t*>(x.out), x.count, coef);
   }
 }
 

@@ -24,16 +24,8 @@ def _dense(t: torch.Tensor, device, name: str):
     return t
 
 
-class ClipPlan:
-    """The gradients of a model as one list, for its global norm and for
-    clipping by it: checked and marshalled once, for buffers that stay where
-    they are from step to step.  The plan keeps the tensors; a call after one
-    was moved raises.
-
-    grads: contiguous CUDA tensors (float32, bfloat16, float16, mixed, of any
-    size) of one device.  out: where clipped gradients go, one tensor of the
-    same type and size for each (each its gradient itself, or apart from all
-    others); None: in place."""
+class _Tensors:
+    """Gradients and where clipped ones go, checked and marshalled."""
 
     def __init__(self, grads, out=None):
         grads = list(grads)
@@ -48,54 +40,82 @@ class ClipPlan:
             _dense(o, self.device, "out")
             if o.dtype != g.dtype or o.shape != g.shape:
                 raise ValueError("an output must have its gradient's type and shape")
-        k = len(grads)
-        self._n = k
-        self._types = (C.c_int32 * k)(*(_type(g.dtype, "grads") for g in grads))
-        self._numel = (C.c_int64 * k)(*(g.numel() for g in grads))
-        self._in = (C.c_void_p * k)(*(g.data_ptr() for g in grads))
-        self._out = (C.c_void_p * k)(*(o.data_ptr() for o in out))
-        self._at = [g.data_ptr() for g in grads]
-        self._out_at = [o.data_ptr() for o in out] if out is not grads else None
-        self._words = int(lib().ps_clip_workspace_bytes(k)) // 8
+        self.n = k = len(grads)
+        self.types = (C.c_int32 * k)(*(_type(g.dtype, "grads") for g in grads))
+        self.numel = (C.c_int64 * k)(*(g.numel() for g in grads))
+        self.at = [g.data_ptr() for g in grads]
+        self.out_at = self.at if out is grads else [o.data_ptr() for o in out]
+        self.ins, self.outs = (C.c_void_p * k)(*self.at), (C.c_void_p * k)(*self.out_at)
 
-    def _check(self, out_at=None):
+
+def _buffers(count: int, device):
+    """The norm, and a workspace of the call's own (a captured call keeps it)."""
+    words = int(lib().ps_clip_workspace_bytes(count)) // 8
+    buf = torch.empty(1 + words, dtype=torch.float64, device=device)
+    return buf[:1], buf.data_ptr() + 8, 8 * words
+
+
+class ClipPlan:
+    """The gradients of a model as one list, for its global norm and for
+    clipping by it: checked once and listed on the device, for buffers that stay
+    where they are from step to step.  The plan keeps the tensors; a call after
+    one was moved raises.  A captured call needs the plan as long as its graph.
+
+    grads: contiguous CUDA tensors (float32, bfloat16, float16, mixed, of any
+    size) of one device.  out: where clipped gradients go, one tensor of the
+    same type and size for each (each its gradient itself, or apart from all
+    others); None: in place."""
+
+    def __init__(self, grads, out=None):
+        t = _Tensors(grads, out)
+        self.grads, self.out, self.device, self._at = t.grads, t.out, t.device, t.at
+        self._out_at = t.out_at if t.out is not t.grads else None
+        host = torch.empty(int(lib().ps_clip_plan_bytes(t.n, t.numel)), dtype=torch.uint8)
+        apart = C.c_int64()
+        check(lib().ps_clip_plan(t.n, t.ins, t.outs, t.numel, t.types, host.data_ptr(), host.numel(), C.byref(apart)))
+        self._apart = apart.value
+        self._list = host.to(self.device)
+        torch.cuda.current_stream(self.device).synchronize()   # there for calls on every stream
+        self._list_at, self._list_bytes = self._list.data_ptr(), host.numel()
+
+    def _run(self, scaling: int, max_norm: float, stream):
         if list(map(torch.Tensor.data_ptr, self.grads)) != self._at or (
-                out_at is not None and list(map(torch.Tensor.data_ptr, self.out)) != out_at):
+                scaling and self._out_at is not None and list(map(torch.Tensor.data_ptr, self.out)) != self._out_at):
             raise RuntimeError("a tensor of the plan has moved: make a new one")
-
-    def _buffers(self):
-        # of its own per call: a captured call keeps the ones it was captured with
-        buf = torch.empty(1 + self._words, dtype=torch.float64, device=self.device)
-        return buf[:1], buf.data_ptr() + 8, 8 * self._words
+        with _On(self.device, stream, (*self.grads, *self.out, self._list) if stream is not None else ()) as st:
+            norm, ws, wsb = _buffers(1, self.device)
+            check(lib().ps_clip_run(self._list_at, self._list_bytes, self._apart, scaling, max_norm, norm.data_ptr(), ws,
+                                    wsb, st))
+        return norm
 
     def norm(self, stream=None) -> torch.Tensor:
         """The global norm of the gradients, float64[1]."""
-        self._check()
-        with _On(self.device, stream, self.grads) as st:
-            norm, ws, wsb = self._buffers()
-            check(lib().ps_grad_norm(self._n, self._in, self._numel, self._types, norm.data_ptr(), ws, wsb, st))
-        return norm
+        return self._run(0, 0.0, stream)
 
     def clip(self, max_norm: float, stream=None) -> torch.Tensor:
         """Write the gradients, scaled by max_norm / norm where the norm is
         larger, to the outputs; returns the norm before, float64[1]."""
-        self._check(self._out_at)
-        with _On(self.device, stream, (*self.grads, *self.out) if stream is not None else ()) as st:
-            norm, ws, wsb = self._buffers()
-            check(lib().ps_clip_grads(self._n, self._in, self._out, self._numel, self._types, max_norm,
-                                      norm.data_ptr(), ws, wsb, st))
-        return norm
+        return self._run(1, max_norm, stream)
 
 
 def grad_norm(grads, stream=None) -> torch.Tensor:
-    """The global norm of a list of gradients, float64[1] (see ClipPlan)."""
-    return ClipPlan(grads).norm(stream)
+    """The global norm of a list of gradients, float64[1] (tensors as in
+    ClipPlan, which is quicker where they stay the same)."""
+    t = _Tensors(grads)
+    with _On(t.device, stream, t.grads) as st:
+        norm, ws, wsb = _buffers(t.n, t.device)
+        check(lib().ps_grad_norm(t.n, t.ins, t.numel, t.types, norm.data_ptr(), ws, wsb, st))
+    return norm
 
 
 def clip_grads(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
     """Clip a list of gradients by their global norm, in place or into out;
-    returns the norm before, float64[1] (see ClipPlan)."""
-    return ClipPlan(grads, out).clip(max_norm, stream)
+    returns the norm before, float64[1] (as ClipPlan.clip)."""
+    t = _Tensors(grads, out)
+    with _On(t.device, stream, (*t.grads, *t.out)) as st:
+        norm, ws, wsb = _buffers(t.n, t.device)
+        check(lib().ps_clip_grads(t.n, t.ins, t.outs, t.numel, t.types, max_norm, norm.data_ptr(), ws, wsb, st))
+    return norm
 
 
 # ---------------------------------------------------------------------------- microscaled 4-bit rows

@@ -236,3 +236,60 @@ def test_a_plan_whose_tensors_moved_is_refused():
     with pytest.raises(RuntimeError, match="moved"):
         plan.clip(1.0)
     plan.norm(), inplace.clip(1.0)
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("sizes,types", SETS)
+def test_norm_and_clip_by_a_plan(sizes, types, offset):
+    say(f"plan of {len(sizes)} tensors, {sum(sizes)} elements, offset {offset}")
+    grads = tensors(sizes, types, 2, std=0.3, offset=offset)
+    before = [g.clone() for g in grads]
+    outs = [torch.full_like(g, 9.0) for g in grads]
+    apart, inplace = ClipPlan(grads, outs), ClipPlan(grads)
+    norm = check_norm(apart.norm(), grads)
+    assert all(bool((o == 9.0).all()) for o in outs)           # the norm alone writes nothing else
+    for max_norm in (norm * 0.37, norm * 1.5):
+        check_norm(apart.clip(max_norm), before)
+        check_scaled(outs, before, norm, max_norm)
+        assert all(torch.equal(g, b) for g, b in zip(grads, before))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    check_norm(apart.clip(norm * 0.5, stream=side), before)
+    side.synchronize()
+    check_scaled(outs, before, norm, norm * 0.5)
+    check_norm(inplace.clip(norm * 0.37), before)
+    check_scaled(grads, before, norm, norm * 0.37)
+    kept = [g.clone() for g in grads]
+    assert float(inplace.clip(norm * 0.37 * 1.01)) <= norm * 0.37 * 1.01
+    assert all(torch.equal(g, k) for g, k in zip(grads, kept))
+
+
+def test_plans_of_mixed_places_nothing_and_one_huge_tensor():
+    # some tensors in place, some apart, neighbours left alone
+    flat = torch.ones(5000, dtype=BF16, device="cuda")
+    far = torch.full((5000,), 3.0, dtype=BF16, device="cuda")
+    spans = [(1, 700), (703, 1), (709, 2000), (3333, 1600)]
+    grads = [flat[a:a + n] for a, n in spans]
+    outs = [g if i % 2 else far[a:a + n] for i, (g, (a, n)) in enumerate(zip(grads, spans))]
+    ClipPlan(grads, outs).clip(1.0)
+    inside = torch.zeros(5000, dtype=torch.long)
+    for i, (a, n) in enumerate(spans):
+        inside[a:a + n] = 1 + i % 2
+    assert bool((far.cpu()[inside != 1] == 3.0).all()) and bool((far.cpu()[inside == 1] < 0.1).all())
+    assert bool((flat.cpu()[inside != 2] == 1.0).all()) and bool((flat.cpu()[inside == 2] < 0.1).all())
+    with pytest.raises(RuntimeError):
+        ClipPlan([flat, flat])
+    with pytest.raises(RuntimeError):
+        ClipPlan([flat[:10]], [flat[5:15]])
+    empty = ClipPlan([flat[:0], far[:0]])
+    assert float(empty.norm()) == 0.0 and float(empty.clip(1.0)) == 0.0
+    with pytest.raises(RuntimeError):
+        ClipPlan([flat]).clip(0.0)
+    x = torch.zeros((1 << 31) + 9, dtype=BF16, device="cuda")
+    x[3], x[-1] = 36.0, 77.0
+    plan = ClipPlan([x])
+    assert float(plan.norm()) == 85.0 and float(plan.clip(17.0)) == 85.0
+    # 17 / 85 to fp32, its products to fp32 and to bf16
+    for at, v in ((3, 36.0), (-1, 77.0)):
+        assert float(x[at]) == float((torch.tensor(v) * torch.tensor(17.0 / 85.0)).to(BF16))
+    assert int((x[: 1 << 31] != 0).sum()) == 1

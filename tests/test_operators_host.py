@@ -127,3 +127,37 @@ def test_new_constants_match_the_header():
     for name in ("PS_F32", "PS_BF16", "PS_F16"):
         assert getattr(_lib, name) == defs[name], name
     assert _lib.PS_NO_PAD == -(2 ** 63)
+
+
+def test_clip_plans_refuse_bad_arguments():
+    L, A, B = _lib.lib(), 0x100000, 0x200000
+    arr = lambda t, *v: (t * len(v))(*v)
+    i64, i32, ptr = C.c_int64, C.c_int32, C.c_void_p
+    assert L.ps_clip_plan_bytes(0, None) == 0 and L.ps_clip_plan_bytes(-1, None) == 0
+    assert L.ps_clip_plan_bytes(1, None) == 0 and L.ps_clip_plan_bytes(2, arr(i64, 5, -1)) == 0
+    assert L.ps_clip_plan_bytes(1, arr(i64, 0)) == 0
+    size = L.ps_clip_plan_bytes(2, arr(i64, 16384, 16385))
+    assert size == 3 * 24
+    host, apart = (C.c_uint8 * 96)(*[0xee] * 96), C.c_int64(-1)
+
+    def plan(grads, outs, numel, types, to=host, nb=size, ap=apart):
+        return L.ps_clip_plan(len(numel), arr(ptr, *grads), None if outs is None else arr(ptr, *outs), arr(i64, *numel),
+                              arr(i32, *types), to, nb, None if ap is None else C.byref(ap))
+
+    ok = ([A, B], [A, 0x400000], [16384, 16385], [F32, BF16])
+    assert plan(*ok) == 0 and apart.value == 2 * 16385
+    assert bytes(host)[size:] == b"\xee" * (96 - size)
+    words = (C.c_uint64 * 9).from_buffer(host)
+    assert list(words) == [A, A, 16384, B, 0x400000, 16384 | BF16 << 32, B + 32768, 0x400000 + 32768, 1 | BF16 << 32]
+    assert plan(*ok, nb=size - 24) == BAD and plan(*ok, to=None) == BAD and plan(*ok, ap=None) == BAD
+    assert plan([A, B], None, *ok[2:]) == BAD
+    assert plan([A, A], [A, A], [10, 10], [F32, F32], nb=48) == BAD        # both write one tensor
+    assert plan([A, B], [A, A + 4], [10, 10], [F32, F32], nb=48) == BAD
+    assert plan([A, B], [A, B], [10, -1], [F32, F32], nb=0) == BAD
+    assert plan([A + 2, B], [A + 2, B], *ok[2:]) == BAD
+    run = lambda p=P(), nb=size, scaling=1, m=1.0, norm=P(0x8000), ws=P(0x4000), wsb=1 << 20: L.ps_clip_run(
+        p, nb, 0, scaling, m, norm, ws, wsb, None)
+    for bad in (dict(p=None), dict(p=P(0x10001)), dict(nb=size - 1), dict(m=0.0), dict(m=float("nan")), dict(norm=None),
+                dict(norm=P(0x8004)), dict(ws=None), dict(ws=P(0x4001))):
+        assert run(**bad) == BAD, bad
+    assert run(wsb=8) == SMALL and run(scaling=0, m=0.0, wsb=8) == SMALL
