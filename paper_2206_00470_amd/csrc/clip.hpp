@@ -146,7 +146,8 @@ __global__ __launch_bounds__(BLOCK) void k_norm_total(const double* __restrict__
 
 struct Coef {
   float unit;   // 1, or 2^-100 where the factor is below it
-  float c;
+  float c;      // (1 too where a factor just below 2^-100 is rounded to it)
+  __device__ __forceinline__ bool is_one() const { return unit == 1.0f && c == 1.0f; }
   __device__ __forceinline__ float operator()(float x) const { return x * unit * c; }
 };
 
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(BLOCK) void k_clip_scale(const List t, const double
   const uint32_t chunks = t.chunks();
   for (uint32_t q = blockIdx.x; q < chunks; q += gridDim.x) {
     const ClipChunk x = t.at(chunks - 1 - q);
-    if (coef.c == 1.0f && x.in == x.out) continue;   // in place, and within the bound
+    if (coef.is_one() && x.in == x.out) continue;   // in place, and within the bound
     if (x.type == 0) chunk_scale<float, NT>(static_cast<const float*>(x.in), static_cast<float*>(x.out), x.count, coef);
     else if (x.type == 1)
       chunk_scale<bf16_t, NT>(static_cast<const bf16_t*>(x.in), static_cast<bf16_t*>(x.out), x.count, coef);

@@ -293,3 +293,17 @@ def test_plans_of_mixed_places_nothing_and_one_huge_tensor():
     for at, v in ((3, 36.0), (-1, 77.0)):
         assert float(x[at]) == float((torch.tensor(v) * torch.tensor(17.0 / 85.0)).to(BF16))
     assert int((x[: 1 << 31] != 0).sum()) == 1
+
+
+@pytest.mark.parametrize("planned", [False, True])
+def test_a_factor_just_below_its_unit_clips_in_place(planned):
+    """Factors below 2^-100 are applied as 2^-100 times the rest; a rest that
+    rounds to 1 leaves a factor of 2^-100, not of 1."""
+    values, far = [2.0 ** 100, 2.0 ** 86], [1.0, 2.0 ** -14]   # norm 2^100 (1 + 2^-29): the rest is 1 - 2^-29
+    x = torch.tensor(values, dtype=F32, device="cuda")
+    out = torch.zeros_like(x)
+    clip = (lambda g, o: ClipPlan(g, o).clip(1.0)) if planned else (lambda g, o: clip_grads(g, 1.0, out=o))
+    check_norm(clip([x], [out]), [x])
+    assert x.tolist() == values and out.tolist() == far
+    clip([x], None)
+    assert x.tolist() == far
