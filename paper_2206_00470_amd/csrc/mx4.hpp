@@ -102,6 +102,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__
   int bad = 0, miss = 0;
   constexpr int VW = 16 / sizeof(OT);
   uint32_t w[U], s[U];
+  float mul[U];   // scale, or 0 for a row of zeros: their codes and scale bytes are 0
   int64_t at[U];
   int col[U];
 #pragma unroll
@@ -113,6 +114,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__
     col[u] = dim;   // nothing to write
     w[u] = 0;
     s[u] = 0;
+    mul[u] = 0.0f;
     if (i < l.n) {
       col[u] = (int)c;
       at[u] = i * out_ld + c;
@@ -122,6 +124,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__
         if constexpr (VW == 8) w[u] = *reinterpret_cast<const uint32_t*>(p);
         else w[u] = *reinterpret_cast<const uint16_t*>(p);
         s[u] = scales[r * blocks_row + c / MX_BLOCK];
+        mul[u] = scale;
       }
     }
   }
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(BLOCK) void k_mx4_embed(const uint8_t* __restrict__
       c[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 3);
     }
 #pragma unroll
-    for (int e = 0; e < VW; ++e) x[e] = c[e / 2][e % 2] * f * scale;
+    for (int e = 0; e < VW; ++e) x[e] = c[e / 2][e % 2] * f * mul[u];
     const int left = dim - col[u];
     if (left >= VW) {
       store_any<OT, VW, NT>(out + at[u], raw_make<OT, VW>(x));

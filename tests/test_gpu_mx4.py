@@ -300,3 +300,23 @@ def test_a_table_used_first_on_two_streams_reports_its_error():
     x.embed(bad, stream=two)
     torch.cuda.synchronize()
     assert x.error() == _lib.PS_ERR_KEY_RANGE and x.error() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("scale", [float("inf"), -float("inf"), float("nan"), -1.0, 1e38, 0.0])
+def test_rows_that_are_not_there_are_zeros_whatever_the_factor(scale, dtype):
+    """Padding and ids outside the table, as Store.embed gives them: +0 in every bit."""
+    dim, word = 45, torch.int32 if dtype == F32 else torch.int16
+    W = random_rows(30, dim, 12)
+    W[5, 3] = float("inf")                                    # a block of NaN, not looked up by an absent row
+    q = mx4_quantize(W.cuda())
+    s = Store(W.cuda(), torch.ones((30, dim), device="cuda"))
+    ids = torch.tensor([-1, 4, 30, -1, 2 ** 40, 5, -3, -1, 0], device="cuda")
+    there = torch.tensor([False, True, False, False, False, True, False, False, True])
+    values = q.dequantize().cpu()
+    for got in (q.embed(ids, scale=scale, dtype=dtype, pad=-1), s.embed(ids, scale=scale, dtype=dtype, pad=-1)):
+        assert not bool(got.view(word)[~there.cuda()].any())
+    got = q.embed(ids, scale=scale, dtype=dtype, pad=-1).cpu()[there]
+    ref = (values[ids.cpu()[there]] * torch.tensor(scale)).to(dtype)
+    assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.nan_to_num(), ref.nan_to_num())
+    assert q.error() == _lib.PS_ERR_KEY_RANGE and s.error() == _lib.PS_ERR_KEY_RANGE
