@@ -7,6 +7,7 @@ in the HIP kernels of ``libadapm_hip.so``.
 from __future__ import annotations
 
 import ctypes as C
+import threading
 
 import torch
 
@@ -120,6 +121,7 @@ def clip_grads(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
 
 # ---------------------------------------------------------------------------- microscaled 4-bit rows
 MX_BLOCK = 32
+_FLAGS = threading.Lock()   # held while a table's error flag is made (of all tables: one that held its own could not be copied)
 
 
 class MX4:
@@ -147,10 +149,22 @@ class MX4:
         self._err = None
         return self
 
+    def _make_flag(self, stream):
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the first embed of a table makes its error flag: call it before a capture")
+        with _FLAGS:
+            if self._err is None:
+                flag = torch.zeros(2, dtype=torch.int32, device=self.device)
+                torch.cuda.current_stream(self.device).synchronize()
+                self._err = flag   # seen by other threads from now on: zero for calls on every stream
+        if stream is not None:
+            self._err.record_stream(stream)
+
     def embed(self, ids: torch.Tensor, scale: float = 1.0, dtype: torch.dtype = torch.float32, pad: int | None = None,
               out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Store.embed from these rows; an id outside them gives zeros and
-        raises the sticky error that error() reports."""
+        raises the sticky error that error() reports.  The first call waits for
+        that error's flag to be cleared, and is refused during a capture."""
         _dev(ids, torch.int64, "ids")
         if ids.device != self.device:
             raise TypeError(f"ids must be on {self.device}")
@@ -164,10 +178,7 @@ class MX4:
     def _lookup(self, ids, n, shape, scale, dtype, pad, out, stream):
         with _On(self.device, stream, (self.codes, self.scales, ids, out, self._err)) as st:
             if ids is not None and self._err is None:
-                if torch.cuda.is_current_stream_capturing():
-                    raise RuntimeError("the first embed of a table makes its error flag: call it before a capture")
-                self._err = torch.zeros(2, dtype=torch.int32, device=self.device)
-                torch.cuda.current_stream(self.device).synchronize()   # zero for calls on every stream
+                self._make_flag(stream)
             ld = self.dim
             if out is None:
                 out = torch.empty((*shape, ld), dtype=dtype, device=self.device)

@@ -1,6 +1,9 @@
 """Microscaled 4-bit rows against the format's definition in 64 bits:
 quantisation bit for bit, lookups bit for bit, products within the rounding of
 fp32 sums."""
+import threading
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -320,3 +323,25 @@ def test_rows_that_are_not_there_are_zeros_whatever_the_factor(scale, dtype):
     ref = (values[ids.cpu()[there]] * torch.tensor(scale)).to(dtype)
     assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.nan_to_num(), ref.nan_to_num())
     assert q.error() == _lib.PS_ERR_KEY_RANGE and s.error() == _lib.PS_ERR_KEY_RANGE
+
+
+def test_a_table_used_first_by_two_threads_reports_its_error():
+    """One thread's first lookup waits behind a long stream for its flag, another
+    thread's lookup on a stream of its own finds an id outside the table."""
+    good, bad = torch.arange(50, device="cuda"), torch.full((3,), 50, dtype=torch.int64, device="cuda")
+    a = torch.randn((8192, 8192), device="cuda")
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    for turn in range(3):
+        x = mx4_quantize(torch.randn((50, 64), device="cuda"))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(one):
+            for _ in range(4):
+                b = a @ a
+        first = threading.Thread(target=lambda: x.embed(good, stream=one))
+        first.start()
+        time.sleep(0.003 * turn)
+        got = x.embed(bad, stream=two)
+        first.join()
+        torch.cuda.synchronize()
+        assert not bool(got.any())
+        assert x.error() == _lib.PS_ERR_KEY_RANGE and x.error() == 0

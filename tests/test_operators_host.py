@@ -1,12 +1,15 @@
 """Refusals of the token-table operators on the host: bad arguments are
 reported before anything is enqueued (no GPU is needed, addresses are never
 followed)."""
+import copy
 import ctypes as C
+import threading
+import time
 
 import pytest
 import torch
 
-from paper_2206_00470_amd import ClipPlan, MX4, _lib
+from paper_2206_00470_amd import ClipPlan, MX4, _lib, operators
 from paper_2206_00470_amd.store import _rows
 
 P = lambda a=0x10000: C.c_void_p(a)
@@ -161,3 +164,56 @@ def test_clip_plans_refuse_bad_arguments():
                 dict(norm=P(0x8004)), dict(ws=None), dict(ws=P(0x4001))):
         assert run(**bad) == BAD, bad
     assert run(wsb=8) == SMALL and run(scaling=0, m=0.0, wsb=8) == SMALL
+
+
+def test_a_quantised_tables_first_lookups_share_one_cleared_flag(monkeypatch):
+    """Two threads look a table up for the first time, the second while the first
+    waits for the flag's zeros: both launches get one flag, after that wait."""
+    x = MX4.__new__(MX4)._set(torch.zeros((4, 16), dtype=torch.uint8), torch.zeros((4, 1), dtype=torch.uint8), 32)
+    ids = torch.zeros(2, dtype=torch.int64)
+    waiting, second, flags, waits = threading.Event(), threading.Event(), [], []
+
+    class On:
+        def __init__(self, *a):
+            pass
+
+        def __enter__(self):
+            second.set() if threading.current_thread().name == "second" else None
+
+        def __exit__(self, *a):
+            pass
+
+    class Stream:
+        def synchronize(self):
+            waits.append(1)
+            waiting.set()
+            second.wait(5)
+            time.sleep(0.3)   # the other thread goes as far as it can
+            assert not flags, "a lookup was launched before the flag was cleared"
+
+    class Lib:
+        def ps_mx4_embed(self, *a):
+            flags.append(a[-2])
+            return _lib.PS_OK
+
+    monkeypatch.setattr(operators, "_On", On)
+    monkeypatch.setattr(operators, "lib", Lib)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream())
+    failed = []
+
+    def look():
+        try:
+            x._lookup(ids, 2, ids.shape, 1.0, torch.float32, None, None, None)
+        except BaseException as e:
+            failed.append(e)
+
+    a, b = threading.Thread(target=look, name="first"), threading.Thread(target=look, name="second")
+    a.start()
+    assert waiting.wait(20)
+    b.start()
+    a.join(20), b.join(20)
+    assert not failed, failed
+    assert len(waits) == 1 and len(flags) == 2 and flags[0] == flags[1] == x._err.data_ptr()
+    assert not x._err.any()
+    assert torch.equal(copy.deepcopy(x).codes, x.codes)       # a table can be copied as it is
