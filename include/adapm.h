@@ -439,7 +439,7 @@ ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, floa
  * ps_embed_grad_workspace_bytes(dim, n) (0: invalid arguments, or n = 0,
  * which needs none).  Staged stores: PS_ERR_UNSUPPORTED. */
 size_t ps_embed_grad_workspace_bytes(int32_t dim, int64_t n);
-ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, double scale, int32_t in_type,
                         const void* dout, int64_t dout_stride, int32_t out_type, void* grad, int64_t grad_stride,
                         int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
 
@@ -449,7 +449,7 @@ ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad,
  * gradient rows, *num_unique (device int32, or pinned host memory) their
  * number U, written once, before the rows are; uniq[U..] and rows[U..] are
  * left as they are.  ps_push takes uniq and rows as they are (fp32, dense). */
-ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, double scale, int32_t in_type,
                              const void* dout, int64_t dout_stride, int32_t out_type, int64_t* uniq, void* rows,
                              int64_t rows_stride, int32_t* num_unique, void* ws, size_t ws_bytes, void* stream);
 

@@ -75,8 +75,8 @@ SIGNATURES = {
     "ps_read_timing": (_i32, [_p, _i32, C.POINTER(C.c_double), C.POINTER(_i64)]),
     "ps_embed": (_i32, [_p, _p, _i64, _i64, _f32, _i32, _p, _i64, _p]),
     "ps_embed_grad_workspace_bytes": (_sz, [_i32, _i64]),
-    "ps_embed_grad": (_i32, [_p, _p, _i64, _i64, _f32, _i32, _p, _i64, _i32, _p, _i64, _i32, _p, _sz, _p]),
-    "ps_embed_grad_rows": (_i32, [_p, _p, _i64, _i64, _f32, _i32, _p, _i64, _i32, _p, _p, _i64, _p, _p, _sz, _p]),
+    "ps_embed_grad": (_i32, [_p, _p, _i64, _i64, C.c_double, _i32, _p, _i64, _i32, _p, _i64, _i32, _p, _sz, _p]),
+    "ps_embed_grad_rows": (_i32, [_p, _p, _i64, _i64, C.c_double, _i32, _p, _i64, _i32, _p, _p, _i64, _p, _p, _sz, _p]),
     "ps_wait_count": (_i32, [_p, _p]),
     "ps_clip_workspace_bytes": (_sz, [_i32]),
     "ps_grad_norm": (_i32, [_i32, _p, _p, _p, _p, _p, _sz, _p]),

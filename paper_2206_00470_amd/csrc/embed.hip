@@ -124,7 +124,7 @@ struct GradCall {
   const int64_t* ids;
   int64_t n;
   int64_t pad;
-  float scale;
+  double scale;
   int32_t in_type;
   const void* dout;
   int64_t in_ld;
@@ -250,7 +250,7 @@ size_t ps_embed_grad_workspace_bytes(int32_t dim, int64_t n) {
   return plan_grad(nullptr, n, dim).bytes;
 }
 
-ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, double scale, int32_t in_type,
                         const void* dout, int64_t dout_stride, int32_t out_type, void* grad, int64_t grad_stride,
                         int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
   return embed_grad(s, GradCall{ids, n, pad, scale, in_type, dout, dout_stride,
@@ -258,7 +258,7 @@ ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad,
                     ws, ws_bytes, static_cast<hipStream_t>(stream));
 }
 
-ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, float scale, int32_t in_type,
+ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, double scale, int32_t in_type,
                              const void* dout, int64_t dout_stride, int32_t out_type, int64_t* uniq, void* rows,
                              int64_t rows_stride, int32_t* num_unique, void* ws, size_t ws_bytes, void* stream) {
   if (!num_unique) return raise(PS_ERR_INVALID, "num_unique is NULL");

@@ -100,10 +100,10 @@ __device__ __forceinline__ void add_old(const GradOut& o, int64_t at, double* x)
 
 template <int VW>
 __device__ __forceinline__ void write_grad_any(const GradOut& o, int64_t row, int col, const double* acc,
-                                               float scale) {
+                                               double scale) {
   double x[VW];
 #pragma unroll
-  for (int e = 0; e < VW; ++e) x[e] = (double)scale * acc[e];
+  for (int e = 0; e < VW; ++e) x[e] = scale * acc[e];
   if (o.accumulate) {
     const int64_t at = row * o.ld + col;
     if (o.type == 0) add_old<float, VW>(o, at, x);
@@ -248,7 +248,7 @@ struct alignas(16) GradMeta {
 // round.
 template <class IT, int VW, int BLK>
 __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __restrict__ dout, int64_t in_ld, int dim,
-                                                      int log_lanes, float scale, GradOut out) {
+                                                      int log_lanes, double scale, GradOut out) {
   constexpr int U = BLK;
   extern __shared__ GradMeta grad_meta[];   // one per group
   const int lanes = 1 << log_lanes;
@@ -311,11 +311,10 @@ __global__ __launch_bounds__(BLOCK) void k_grad_merge(GradRuns g, const IT* __re
       if (i >= mine) return;   // nothing of this group's follows
       const bool ends = k[i + 1] != k[i];
       if (ends && start == p + i && !came_in && !out.accumulate) {
-        // a token that comes once: its product in fp32 is the fp64 one (of two
-        // 24-bit numbers, exact) rounded
+        // a token that comes once: no sum
         float y[VW];
 #pragma unroll
-        for (int e = 0; e < VW; ++e) y[e] = scale * raw_get<IT, VW>(x[i], e);
+        for (int e = 0; e < VW; ++e) y[e] = (float)(scale * (double)raw_get<IT, VW>(x[i], e));
         if (active) write_row_any<VW>(out, g.seg_off ? (int64_t)u : (int64_t)k[i], col, y);
         start = p + i + 1;
         ++u;
@@ -415,7 +414,7 @@ __device__ __forceinline__ int32_t last_block(const GradRuns& g, uint32_t key, i
 // The runs over three blocks and more: partial of the first block, of the
 // blocks up to the first folded ones, the folds, and the blocks after them.
 __global__ __launch_bounds__(BLOCK) void k_grad_finish(GradRuns g, int dim, int slices,
-                                                       const double* __restrict__ fold, float scale, GradOut out) {
+                                                       const double* __restrict__ fold, double scale, GradOut out) {
   __shared__ double smem[BLOCK];
   const int64_t items = (int64_t)*g.split_count * slices;
   for (int64_t e = blockIdx.x; e < items; e += gridDim.x) {

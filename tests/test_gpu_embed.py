@@ -514,3 +514,32 @@ def test_the_lowest_id_is_outside_the_table(n, pad):
     x = mx4_quantize(W)
     got = x.embed(ids.cuda(), pad=pad)
     assert bool((got[n // 2] == 0).all()) and x.error() == _lib.PS_ERR_KEY_RANGE and x.error() == 0
+
+
+@pytest.mark.parametrize("scale", [1.7, 300 ** 0.5, -1.0 / 3.0, 1e-50, 1.0 + 2.0 ** -30])
+@pytest.mark.parametrize("form", ["dense", "rows", "added"])
+@pytest.mark.parametrize("K,d,n", [(4000, 33, 900), (200, 20, 6000), (3, 64, 30_000), (90_000, 24, 70_001)])
+def test_the_gradients_factor_keeps_its_64_bits(K, d, n, form, scale):
+    """Tokens that come once, a few times and over many blocks: what remains is
+    the one rounding to fp32."""
+    s = Store(torch.zeros((K, d), device="cuda"), torch.ones((K, d), device="cuda"))
+    ids = make_ids(K, n, 500 + n, "uniform")
+    dout = torch.randn((n, d), generator=torch.Generator().manual_seed(501))
+    if scale == 1e-50:
+        dout = (dout.abs() + 1) * 1e30                        # the factor is 0 in 32 bits, its products are not
+    ref, mag, count = plain_grad(K, ids, dout, scale, None)
+    say(f"factor {scale} {form} K={K} d={d} n={n}")
+    if form == "rows":
+        uniq, got = s.embed_grad_rows(ids.cuda(), dout.cuda(), scale=scale)
+        ref, mag, count = ref[uniq.cpu()], mag[uniq.cpu()], count[uniq.cpu()]
+    elif form == "dense":
+        got = s.embed_grad(ids.cuda(), dout.cuda(), scale=scale)
+    else:
+        old = torch.randn((K, d), generator=torch.Generator().manual_seed(502)) * (count > 0)[:, None] * 1e-3
+        ref, mag, count = ref + old.double(), mag + old.double().abs(), count + 1
+        got = s.embed_grad(ids.cuda(), dout.cuda(), scale=scale, out=old.cuda(), accumulate=True)
+    # both sums and the products with the factor in 64 bits, as in check_grad; rounded to fp32 once
+    tol = 2 * (count.double()[:, None] + 2) * 2.0 ** -53 * mag + 2.0 ** -24 * (1 + 2.0 ** -20) * ref.abs() + TINY[F32]
+    bad = ((got.double().cpu() - ref).abs() > tol).sum()
+    assert int(bad) == 0, f"{int(bad)} of {got.numel()} off"
+    assert s.error() == 0
