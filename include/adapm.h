@@ -433,11 +433,11 @@ ps_status ps_embed(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, floa
  * are summed in fp64 in a fixed order (the same inputs give the same bits),
  * scaled (and added) in fp64, rounded to fp32 and then to the type of grad.
  * Reads no table row and changes none.  Ids outside the table take no part
- * and raise the sticky error.  dout: device [n][dim], row stride dout_stride;
- * grad: device [num_keys][dim], row stride grad_stride; no element of it may
- * be one of dout or of the table.  Workspace:
- * ps_embed_grad_workspace_bytes(dim, n) (0: invalid arguments, or n = 0,
- * which needs none).  Staged stores: PS_ERR_UNSUPPORTED. */
+ * and raise the sticky error.  dout: device [n][dim], row stride dout_stride
+ * (0: one row for all ids); grad: device [num_keys][dim], row stride
+ * grad_stride; no element of it may be one of dout or of the table.
+ * Workspace: ps_embed_grad_workspace_bytes(dim, n) (0: invalid arguments, or
+ * n = 0, which needs none).  Staged stores: PS_ERR_UNSUPPORTED. */
 size_t ps_embed_grad_workspace_bytes(int32_t dim, int64_t n);
 ps_status ps_embed_grad(ps_store* s, const int64_t* ids, int64_t n, int64_t pad, double scale, int32_t in_type,
                         const void* dout, int64_t dout_stride, int32_t out_type, void* grad, int64_t grad_stride,

@@ -156,7 +156,8 @@ ps_status embed_grad(ps_store* s, const GradCall& c, void* ws, size_t ws_bytes, 
   if (ps_status r = check_count(c.n)) return r;
   if (ps_status r = check_type(c.in_type)) return r;
   if (ps_status r = check_type(c.out.type)) return r;
-  if (c.in_ld < t.dim || c.out.ld < t.dim) return raise(PS_ERR_INVALID, "a row stride is smaller than dim %d", t.dim);
+  if ((c.in_ld < t.dim && c.in_ld != 0) || c.out.ld < t.dim)   // (0: one row for all ids)
+    return raise(PS_ERR_INVALID, "a row stride is smaller than dim %d", t.dim);
   if (!c.out.p) return raise(PS_ERR_INVALID, "grad is NULL");
   const bool rows = c.num_unique != nullptr;
   const int ib = type_bytes(c.in_type), ob = type_bytes(c.out.type);

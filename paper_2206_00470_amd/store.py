@@ -316,24 +316,31 @@ class Store:
 
     def _grad_args(self, ids, dout):
         n = self._ids(ids)
-        rows, ld = _rows(dout, self.dim, self.W.device, "dout")
+        if not dout.is_contiguous() and dout.numel() and all(
+                stride == 0 or size == 1 for size, stride in zip(dout.shape[:-1], dout.stride())):
+            # one row for every id, as the backward of a sum gives it
+            count, dout = dout.numel() // dout.shape[-1], dout[(0,) * (dout.dim() - 1)].contiguous()
+            rows, ld = count * _rows(dout, self.dim, self.W.device, "dout")[0], 0
+        else:
+            rows, ld = _rows(dout, self.dim, self.W.device, "dout")
         if rows != n:
             raise ValueError("dout must have one row per id")
         nbytes = int(lib().ps_embed_grad_workspace_bytes(self.dim, n)) if n else 0
         # a workspace of its own per call: a captured call keeps the one it was captured with
-        return n, ld, _type(dout.dtype, "dout"), torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.W.device)
+        return n, dout, ld, _type(dout.dtype, "dout"), torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.W.device)
 
     def embed_grad(self, ids: torch.Tensor, dout: torch.Tensor, scale: float = 1.0, pad: int | None = None,
                    dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, accumulate: bool = False,
                    stream=None) -> torch.Tensor:
         """Gradient of embed as a dense [num_keys, dim] tensor: row v holds
-        scale times the sum of dout's rows whose id is v.  out: the tensor to
+        scale times the sum of dout's rows whose id is v.  dout: equidistant
+        rows, or one row broadcast to all ids.  out: the tensor to
         write (its rows without an id become zero) or, with accumulate, to add
         to."""
         if accumulate and out is None:
             raise ValueError("accumulate needs the gradient to add to (out)")
         with _On(self.W.device, stream, (ids, dout, out)) as st:
-            n, ld, kind, ws = self._grad_args(ids, dout)
+            n, dout, ld, kind, ws = self._grad_args(ids, dout)
             out_ld = self.dim
             if out is None:
                 out = torch.empty((self.num_keys, self.dim), dtype=dtype, device=self.W.device)
@@ -355,7 +362,7 @@ class Store:
         with _On(self.W.device, stream, (ids, dout)) as st:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("embed_grad_rows waits for the number of rows: not during a capture")
-            n, ld, kind, ws = self._grad_args(ids, dout)
+            n, dout, ld, kind, ws = self._grad_args(ids, dout)
             uniq = torch.empty(n, dtype=torch.int64, device=self.W.device)
             rows = torch.empty((n, self.dim), dtype=dtype, device=self.W.device)
             # the number comes straight to host memory: no copy to wait for behind the kernels

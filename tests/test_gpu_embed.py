@@ -543,3 +543,38 @@ def test_the_gradients_factor_keeps_its_64_bits(K, d, n, form, scale):
     bad = ((got.double().cpu() - ref).abs() > tol).sum()
     assert int(bad) == 0, f"{int(bad)} of {got.numel()} off"
     assert s.error() == 0
+
+
+@pytest.mark.parametrize("gin", [F32, BF16])
+@pytest.mark.parametrize("K,d,n", [(300, 33, 77), (50, 64, 9001), (7, 1, 20)])
+def test_gradients_broadcast_along_their_rows(K, d, n, gin):
+    """One row for every id, as the backward of a sum gives it: strides of 0."""
+    s = Store(torch.zeros((K, d), device="cuda"), torch.ones((K, d), device="cuda"))
+    ids = make_ids(K, n, 600)
+    row = torch.randn(d, generator=torch.Generator().manual_seed(601)).to(gin)
+    one = torch.tensor(0.37).to(gin)
+    wide = torch.stack([row, row * 2], dim=1)                 # a row whose elements are two apart
+    for dout, same in ((row.cuda().expand(n, d), row), (one.cuda().expand(n, d), one.expand(d)),
+                       (one.cuda().expand(1, n, d), one.expand(d)), (wide.cuda()[:, 1].expand(n, d), wide[:, 1])):
+        at = ids.cuda().view(dout.shape[:-1])
+        ref, mag, count = plain_grad(K, ids, same.expand(n, d), 1.3, None)
+        check_grad(s.embed_grad(at, dout, scale=1.3), ref, mag, count, F32)
+        uniq, rows = s.embed_grad_rows(at, dout, scale=1.3)
+        assert torch.equal(uniq.cpu(), torch.nonzero(count)[:, 0])
+        check_grad(rows, ref[count > 0], mag[count > 0], count[count > 0], F32)
+    # through a sum's own backward
+    x = s.embed(ids.cuda(), dtype=gin).requires_grad_()
+    dx = torch.autograd.grad(x.sum(), x)[0]
+    check_grad(s.embed_grad(ids.cuda(), dx), *plain_grad(K, ids, torch.ones((n, d), dtype=gin), 1.0, None), F32)
+    assert s.error() == 0
+    # rows that lie over each other otherwise, and outputs that do, are refused
+    zeros = torch.zeros((n, d), device="cuda")
+    with pytest.raises(PSError):
+        s.embed_grad(ids.cuda(), zeros, out=torch.zeros(d, device="cuda").expand(K, d))
+    if d > 1:
+        with pytest.raises(PSError):
+            s.embed_grad(ids.cuda(), torch.zeros(n * d, device="cuda").as_strided((n, d), (d - 1, 1)))
+        with pytest.raises(TypeError):
+            s.embed_grad(ids.cuda(), torch.zeros((n, 1), device="cuda").expand(n, d))
+    with pytest.raises(TypeError):
+        s.embed_grad(ids.cuda(), row.expand(n, d))
