@@ -456,6 +456,7 @@ ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t
 /* Waits on the host for a number that a call above writes to pinned host
  * memory: until *count is not negative.  Set it to a negative number before
  * that call.  PS_ERR_INVALID where the stream's work ends and leaves it so.
+ * A wait longer than 2 ms leaves the processor to others, in naps of 20 us.
  * Not during a capture of the stream. */
 ps_status ps_wait_count(const int32_t* count, void* stream);
 

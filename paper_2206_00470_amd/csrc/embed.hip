@@ -2,6 +2,8 @@
 #include "embed.hpp"
 
 #include <algorithm>
+#include <chrono>
+#include <thread>
 
 #include "internal.hpp"
 #include "rules.hpp"
@@ -270,20 +272,25 @@ ps_status ps_embed_grad_rows(ps_store* s, const int64_t* ids, int64_t n, int64_t
 
 ps_status ps_wait_count(const int32_t* count, void* stream) {
   if (!count) return raise(PS_ERR_INVALID, "count is NULL");
-  // (the stream is asked seldom, some 30 us apart: the number is mostly there before)
-  for (uint32_t i = 1; __atomic_load_n(count, __ATOMIC_ACQUIRE) < 0; ++i) {
-    if (i % 1024 != 0) {
-      __builtin_ia32_pause();
-      continue;
-    }
+  // The number is mostly there within some 100 us, and a nap ends up to 70 us late.  Behind a stream
+  // that has much to do before the call, the processor is left to others.
+  using clock = std::chrono::steady_clock;
+  constexpr std::chrono::microseconds SPIN(2000), NAP(20);
+  const auto there = [&] { return __atomic_load_n(count, __ATOMIC_ACQUIRE) >= 0; };
+  const auto start = clock::now();
+  while (!there()) {
+    if (clock::now() - start < SPIN)
+      for (int i = 0; i < 1024 && !there(); ++i) __builtin_ia32_pause();   // some 30 us between two looks at the stream
+    else
+      std::this_thread::sleep_for(NAP);
+    if (there()) break;   // (to ask a stream takes some 20 us)
     const hipError_t e = hipStreamQuery(static_cast<hipStream_t>(stream));
     if (e == hipErrorNotReady) {
       (void)hipGetLastError();   // no error, and none that a later call should report
       continue;
     }
     RAISE_HIP(e);
-    if (__atomic_load_n(count, __ATOMIC_ACQUIRE) < 0)
-      return raise(PS_ERR_INVALID, "the stream is through and count is still negative");
+    if (!there()) return raise(PS_ERR_INVALID, "the stream is through and count is still negative");
   }
   return PS_OK;
 }

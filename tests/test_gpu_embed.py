@@ -1,6 +1,8 @@
 """The token table's lookup and its gradient against plain forms in 64 bits:
 every store layout and element type, odd widths and counts, strides, padding,
 hot ids, the two forms of the gradient and accumulation."""
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -578,3 +580,22 @@ def test_gradients_broadcast_along_their_rows(K, d, n, gin):
             s.embed_grad(ids.cuda(), torch.zeros((n, 1), device="cuda").expand(n, d))
     with pytest.raises(TypeError):
         s.embed_grad(ids.cuda(), row.expand(n, d))
+
+
+def test_a_long_wait_for_the_number_of_rows_leaves_the_processor():
+    K, d, n = 500, 8, 100
+    s = Store(torch.zeros((K, d), device="cuda"), torch.ones((K, d), device="cuda"))
+    ids, dout = make_ids(K, n, 700), torch.randn((n, d), generator=torch.Generator().manual_seed(701))
+    di, dd, a = ids.cuda(), dout.cuda(), torch.randn((8192, 8192), device="cuda")
+    s.embed_grad_rows(di, dd)
+    torch.cuda.synchronize()
+    for _ in range(15):
+        b = a @ a                                              # some 10 ms each
+    at, used = time.monotonic(), time.thread_time()
+    uniq, rows = s.embed_grad_rows(di, dd)
+    waited, used = time.monotonic() - at, time.thread_time() - used
+    say(f"waited {waited * 1e3:.1f} ms, {used * 1e3:.1f} of them at work")
+    assert waited > 0.03 and used < waited / 2
+    ref, mag, count = plain_grad(K, ids, dout, 1.0, None)
+    assert torch.equal(uniq.cpu(), torch.nonzero(count)[:, 0])
+    check_grad(rows, ref[count > 0], mag[count > 0], count[count > 0], F32)
