@@ -40,7 +40,12 @@ def _type(dtype, name: str) -> int:
 
 
 def _pad(pad) -> int:
-    return _lib.PS_NO_PAD if pad is None else int(pad)
+    if pad is None:
+        return _lib.PS_NO_PAD
+    n = pad if type(pad) is int else int(pad) if pad == pad else 0
+    if not -0x8000000000000000 < n < 0x8000000000000000 or n is not pad and n != pad:   # (the lowest: there is none)
+        raise ValueError(f"pad must be a 64-bit number above the lowest, not {pad}")
+    return n
 
 
 def _rows(t: torch.Tensor, cols: int, device, name: str):

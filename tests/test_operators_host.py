@@ -10,7 +10,7 @@ import pytest
 import torch
 
 from paper_2206_00470_amd import ClipPlan, MX4, _lib, operators
-from paper_2206_00470_amd.store import _rows
+from paper_2206_00470_amd.store import _pad, _rows
 
 P = lambda a=0x10000: C.c_void_p(a)
 BAD, BIG, SMALL = _lib.PS_ERR_INVALID, _lib.PS_ERR_UNSUPPORTED, _lib.PS_ERR_WORKSPACE
@@ -217,3 +217,17 @@ def test_a_quantised_tables_first_lookups_share_one_cleared_flag(monkeypatch):
     assert len(waits) == 1 and len(flags) == 2 and flags[0] == flags[1] == x._err.data_ptr()
     assert not x._err.any()
     assert torch.equal(copy.deepcopy(x).codes, x.codes)       # a table can be copied as it is
+
+
+@pytest.mark.parametrize("pad", [1 << 63, -(1 << 63) - 1, (1 << 64) + 5, -(1 << 63), 1.5, float("nan")])
+def test_pads_that_no_id_can_have_are_refused(pad):
+    """An argument of 64 bits would take such a pad for another number, the
+    lowest one for "no padding"."""
+    with pytest.raises(ValueError, match="pad"):
+        _pad(pad)
+
+
+def test_pads_reach_the_kernels_as_they_are():
+    assert _pad(None) == NOPAD
+    for pad in (0, -1, 7, (1 << 63) - 1, -(1 << 63) + 1, 4.0, torch.tensor(3)):
+        assert _pad(pad) == pad and type(_pad(pad)) is int
