@@ -60,7 +60,10 @@ class ClipPlan:
     """The gradients of a model as one list, for its global norm and for
     clipping by it: checked once and listed on the device, for buffers that stay
     where they are from step to step.  The plan keeps the tensors; a call after
-    one was moved raises.  A captured call needs the plan as long as its graph.
+    one was moved raises.  A program that makes its gradients anew each step
+    (and so would go on clipping the old ones, which the plan holds) takes
+    clip_grads.  Made before a capture; a captured call needs the plan as long
+    as its graph.
 
     grads: contiguous CUDA tensors (float32, bfloat16, float16, mixed, of any
     size) of one device.  out: where clipped gradients go, one tensor of the
@@ -69,6 +72,9 @@ class ClipPlan:
 
     def __init__(self, grads, out=None):
         t = _Tensors(grads, out)
+        with torch.cuda.device(t.device):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a plan copies its list and waits for it: make it before a capture")
         self.grads, self.out, self.device, self._at = t.grads, t.out, t.device, t.at
         self._out_at = t.out_at if t.out is not t.grads else None
         host = torch.empty(int(lib().ps_clip_plan_bytes(t.n, t.numel)), dtype=torch.uint8)

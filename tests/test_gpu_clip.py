@@ -307,3 +307,23 @@ def test_a_factor_just_below_its_unit_clips_in_place(planned):
     assert x.tolist() == values and out.tolist() == far
     clip([x], None)
     assert x.tolist() == far
+
+
+def test_a_plan_is_not_made_during_a_capture():
+    """Its list is copied and waited for: refused before it breaks the capture,
+    which goes on."""
+    grads = tensors([500, 77], [F32, BF16], 7)
+    twice = torch.empty_like(grads[0])
+    torch.cuda.synchronize()
+    G = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(G):
+        with pytest.raises(RuntimeError, match="capture"):
+            ClipPlan(grads)
+        torch.mul(grads[0], 2.0, out=twice)
+        norm = grad_norm(grads)                                # a call without a plan can be captured
+    for r in range(3):
+        grads[0].fill_(r + 1.0), twice.zero_()
+        G.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(twice, grads[0] * 2.0)
+        check_norm(norm, grads)
