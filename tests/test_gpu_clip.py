@@ -327,3 +327,13 @@ def test_a_plan_is_not_made_during_a_capture():
         torch.cuda.synchronize()
         assert torch.equal(twice, grads[0] * 2.0)
         check_norm(norm, grads)
+
+
+@pytest.mark.parametrize("offset", [0, 1, 3])
+@pytest.mark.parametrize("sizes,types", SETS)
+def test_gradients_within_the_bound_stay_without_a_plan(sizes, types, offset):
+    grads = tensors(sizes, types, 8, std=0.3, offset=offset)
+    kept = [g.clone() for g in grads]
+    norm = plain_norm(kept)
+    check_norm(clip_grads(grads, norm * 1.01), kept)
+    assert all(torch.equal(g, k) for g, k in zip(grads, kept))
