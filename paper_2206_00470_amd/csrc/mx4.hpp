@@ -230,17 +230,16 @@ __device__ __forceinline__ void mx_stage(const MxTile& t, int k0, int blocks_row
   }
 }
 
-// SW words of a row's scale bytes from block k0 on, 1 where they are beyond its end.
-template <int SW>
-__device__ __forceinline__ void mx_scales(const MxTile& t, int row, int k0, int blocks_row, uint32_t (&s)[SW]) {
+// A row's scale bytes from block k0 on, two words, 1 where they are beyond its end.
+__device__ __forceinline__ void mx_scales(const MxTile& t, int row, int k0, int blocks_row, uint32_t (&s)[2]) {
   const uint8_t* p = t.scales + (uint32_t)((row < t.last ? row : t.last) * blocks_row + k0);
   const int left = blocks_row - k0;
-  if (left >= 4 * SW) {
-    __builtin_memcpy(s, p, 4 * SW);
+  if (left >= 8) {
+    __builtin_memcpy(s, p, 8);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < SW; ++i) {
+  for (int i = 0; i < 2; ++i) {
     const int have = left - 4 * i;   // of the word's bytes, where below 4
     s[i] = 0x7f7f7f7fu;
     if (have >= 4) {
@@ -300,8 +299,7 @@ __global__ __launch_bounds__(BLOCK, WQ * QT + WT * TT <= 9 ? 4 : 3) void k_mx4_p
   constexpr int RA = WQ * QT * 32, RB = WT * TT * 32;   // rows of the workgroup's tile
   constexpr size_t kStage = (RA + RB) * 8 * sizeof(words4), kOut = WAVES_PER_BLOCK * 32 * PITCH * sizeof(OT);
   __shared__ words4 lds[(kStage > kOut ? kStage : kOut) / sizeof(words4)];
-  constexpr int SW = 2;   // words of scales staged together
-  __shared__ uint32_t scales[SW][RA + RB];
+  __shared__ uint32_t scales[2][RA + RB];   // of the eight staged blocks
   const int w = threadIdx.x / WAVE, l = lane_id();
   uint32_t tb, tq;
   mx_tile(tiles_q, tiles_b, tb, tq);
@@ -339,33 +337,29 @@ __global__ __launch_bounds__(BLOCK, WQ * QT + WT * TT <= 9 ? 4 : 3) void k_mx4_p
                                                                     (int)xa[q]);
   };
   constexpr int SR = (RA + RB + BLOCK - 1) / BLOCK;   // rows whose scales a thread brings
-  uint32_t sc[SR][SW];
+  uint32_t sc[SR][2];
   auto stage = [&](int k0) {
     if (k0 > 0) __syncthreads();
     mx_stage<RB>(tbl, k0, blocks_row, sb);
     mx_stage<RA>(ta, k0, blocks_row, sa);
-    if (k0 % (4 * SW) == 0) {
 #pragma unroll
-      for (int i = 0; i < SR; ++i) {
-        const int row = i * BLOCK + threadIdx.x;
-        if (row < RA) mx_scales(ta, row, k0, blocks_row, sc[i]);
-        else if (row < RA + RB) mx_scales(tbl, row - RA, k0, blocks_row, sc[i]);
-      }
+    for (int i = 0; i < SR; ++i) {
+      const int row = i * BLOCK + threadIdx.x;
+      if (row < RA) mx_scales(ta, row, k0, blocks_row, sc[i]);
+      else if (row < RA + RB) mx_scales(tbl, row - RA, k0, blocks_row, sc[i]);
     }
-    if (k0 % (4 * SW) == 0) {
 #pragma unroll
-      for (int i = 0; i < SR; ++i)
+    for (int i = 0; i < SR; ++i)
 #pragma unroll
-        for (int q = 0; q < SW; ++q)
-          if (i * BLOCK + (int)threadIdx.x < RA + RB) scales[q][i * BLOCK + threadIdx.x] = sc[i][q];
-    }
+      for (int q = 0; q < 2; ++q)
+        if (i * BLOCK + (int)threadIdx.x < RA + RB) scales[q][i * BLOCK + threadIdx.x] = sc[i][q];
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
   int k0 = 0;
   for (; k0 + 8 <= blocks_row; k0 += 8) {
     stage(k0);
-    const uint32_t* s = scales[k0 % (4 * SW) / 4 + half];
+    const uint32_t* s = scales[half];
 #pragma unroll
     for (int t = 0; t < TT; ++t) xb[t] = s[RA + wb + t * 32 + r];
 #pragma unroll
@@ -378,10 +372,9 @@ __global__ __launch_bounds__(BLOCK, WQ * QT + WT * TT <= 9 ? 4 : 3) void k_mx4_p
   if (k0 < blocks_row) {   // up to seven blocks, halved between the lanes below 32 and above
     const int rem = blocks_row - k0, per = (rem + 1) / 2;
     stage(k0);
-    const int w0 = k0 % (4 * SW) / 4;
     // four bytes from byte 0 or `per` (at most 4) of the eight
     auto scale_word = [&](int row) {
-      return (uint32_t)(((uint64_t)scales[w0 + 1][row] << 32 | scales[w0][row]) >> (8 * per * half));
+      return (uint32_t)(((uint64_t)scales[1][row] << 32 | scales[0][row]) >> (8 * per * half));
     };
 #pragma unroll
     for (int t = 0; t < TT; ++t) xb[t] = scale_word(RA + wb + t * 32 + r);
