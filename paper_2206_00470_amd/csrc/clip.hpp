@@ -12,8 +12,9 @@
 // memory: one launch for the norm and one for the scaling, however many tensors
 // there are.  A call without a plan carries its tensors' addresses in the
 // launches' arguments, CLIP_TENSORS at a time: nothing is copied to the device
-// (a call on 397 tensors of 26,610 floats in all 43 us with a plan, 75 without, on
-// 291 of 500M bf16 values 518 and 525).
+// (a plan's call and one of ps_clip_grads, us: 397 tensors of 26,610 floats in all
+// 45 and 45, of 10.6M floats 44 and 66, 291 of 500M bf16 values 511 and 523; from
+// Python the latter also checks each tensor anew, 427, 409 and 527).
 // Each workgroup of the norm leaves one
 // partial sum; each workgroup of the scaling adds all of them up again by
 // itself, in one order, instead of waiting for another launch to do so.
@@ -193,7 +194,8 @@ __device__ __forceinline__ void chunk_scale(const T* p, T* o, int64_t count, Coe
 // writes past the caches.  Measured without a plan, 500M bf16 values in 291 tensors: 567 us
 // through the caches, 528 past them (174 of it the norm, 5.7 TB/s read; 5.6 TB/s
 // read and written by the rest), 536 in the norm's order; 200M fp32 in 400 481,
-// 444 and 450; in place 581 and, in the norm's order, 590.
+// 444 and 450; in place 571 (556 by a plan; 581 and, in the norm's order, 590 when
+// both were timed).
 template <bool NT, class List>
 __global__ __launch_bounds__(BLOCK) void k_clip_scale(const List t, const double* __restrict__ part, int64_t parts,
                                                       double max_norm, double* __restrict__ norm) {

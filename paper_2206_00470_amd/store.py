@@ -303,9 +303,10 @@ class Store:
     def embed(self, ids: torch.Tensor, scale: float = 1.0, dtype: torch.dtype = torch.float32, pad: int | None = None,
               out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Lookup with scaling: scale * W[ids] as ids.shape + (dim,) of dtype
-        (float32, bfloat16, float16); rows of zeros where ids == pad.  An id
-        outside the table gives zeros and raises the sticky error.  out:
-        equidistant rows, in place of a new tensor (dtype is then its own)."""
+        (float32, bfloat16, float16), scale rounded to float32; rows of zeros
+        where ids == pad.  An id outside the table gives zeros and raises the
+        sticky error.  out: equidistant rows apart from the table, in place of
+        a new tensor (dtype is then its own)."""
         n = self._ids(ids)
         with _On(self.W.device, stream, (ids, out)) as st:
             ld = self.dim
@@ -339,9 +340,9 @@ class Store:
                    stream=None) -> torch.Tensor:
         """Gradient of embed as a dense [num_keys, dim] tensor: row v holds
         scale times the sum of dout's rows whose id is v.  dout: equidistant
-        rows, or one row broadcast to all ids.  out: the tensor to
-        write (its rows without an id become zero) or, with accumulate, to add
-        to."""
+        rows, or one row broadcast to all ids.  out: the tensor to write (its
+        rows without an id become zero) or, with accumulate, to add to; apart
+        from dout and the table."""
         if accumulate and out is None:
             raise ValueError("accumulate needs the gradient to add to (out)")
         with _On(self.W.device, stream, (ids, dout, out)) as st:
@@ -363,7 +364,8 @@ class Store:
         """The same gradient as merged rows: (uniq, rows), the distinct ids in
         ascending order and their gradient rows, as push takes them.  Waits
         for the number of distinct ids, not for the rows: they belong to the
-        call's stream."""
+        call's stream.  Both are the front of buffers with room for all ids:
+        clone them where few distinct ones are kept for long."""
         with _On(self.W.device, stream, (ids, dout)) as st:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("embed_grad_rows waits for the number of rows: not during a capture")
