@@ -599,3 +599,39 @@ def test_a_long_wait_for_the_number_of_rows_leaves_the_processor():
     ref, mag, count = plain_grad(K, ids, dout, 1.0, None)
     assert torch.equal(uniq.cpu(), torch.nonzero(count)[:, 0])
     check_grad(rows, ref[count > 0], mag[count > 0], count[count > 0], F32)
+
+
+@pytest.mark.parametrize("n", [8192, 20_000, 150_000])
+def test_captured_gradients_of_every_sort(n):
+    """The dense gradient, one added to, and one of a broadcast row, captured
+    together at the sizes of each sort; replayed beside eager calls."""
+    K, d = 6000, 40
+    s = Store(torch.zeros((K, d), device="cuda"), torch.ones((K, d), device="cuda"))
+    ids, dout, row = make_ids(K, n, 800).cuda(), torch.randn((n, d), device="cuda"), torch.randn(d, device="cuda")
+    a, b, c = (torch.zeros((K, d), device="cuda") for _ in range(3))
+
+    def calls(a, b, c):
+        s.embed_grad(ids, dout, scale=1.1, pad=7, out=a)
+        s.embed_grad(ids, dout, scale=1.1, pad=7, out=b, accumulate=True)
+        s.embed_grad(ids, row.expand(n, d), pad=7, out=c)
+
+    calls(a, b, c)
+    torch.cuda.synchronize()
+    G = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(G):
+        calls(a, b, c)
+    for r in range(4):
+        ids.copy_(make_ids(K, n, 810 + r, "same" if r == 2 else "zipf"))
+        dout.normal_(), row.normal_()
+        old = torch.randn((K, d), device="cuda")
+        a.fill_(5.0), b.copy_(old), c.fill_(5.0)
+        G.replay()
+        x, y, z = torch.empty_like(a), old.clone(), torch.empty_like(c)
+        calls(x, y, z)
+        s.embed_grad_rows(ids, dout)
+        torch.cuda.synchronize()
+        for got, ref in ((a, x), (b, y), (c, z)):
+            assert np.array_equal(bits(got), bits(ref))
+        ref, mag, count = plain_grad(K, ids.cpu(), dout.cpu(), 1.1, 7)
+        check_grad(a, ref, mag, count, F32)
+    assert s.error() == 0
